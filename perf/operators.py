@@ -35,9 +35,9 @@ def listed():
         return dict(name=name, kind="checkpoint", rows=rows, width=width, dtype=dtype,
                     transposed=transposed)
 
-    def linear(name, tokens, outputs, inputs, dtype, out, bias=True):
+    def linear(name, tokens, outputs, inputs, dtype, out, fast, bias=True):
         return dict(name=name, kind="linear", tokens=tokens, outputs=outputs, inputs=inputs,
-                    dtype=dtype, out=out, bias=bias)
+                    dtype=dtype, out=out, fast=fast, bias=bias)
 
     def gradient(name, workers, tokens, outputs, inputs, dtype):
         return dict(name=name, kind="gradient", workers=workers, tokens=tokens, outputs=outputs,
@@ -59,11 +59,12 @@ def listed():
         # a layer's weights after an update, for the input gradient's product
         checkpoint("checkpoint_8192x8192_transposed", 8192, 8192, "bfloat16", True),
         # a single token through a layer: bound by the weights' bytes
-        linear("linear_token_4096x4096", 1, 4096, 4096, "bfloat16", "bfloat16"),
+        linear("linear_token_4096x4096", 1, 4096, 4096, "bfloat16", "bfloat16", False),
         # a ragged batch through an odd layer, the result in 32 bits
-        linear("linear_777x1000x1500", 777, 1000, 1500, "float32", "float32"),
-        # the largest layer and batch
-        linear("linear_16384x8192x8192", 16384, 8192, 8192, "bfloat16", "bfloat16", False),
+        linear("linear_777x1000x1500", 777, 1000, 1500, "float32", "float32", False),
+        # the largest layer and batch, on the 8-bit instruction (its sums are narrower than 32 bits,
+        # which 16-bit results hardly show)
+        linear("linear_16384x8192x8192", 16384, 8192, 8192, "bfloat16", "bfloat16", True, False),
         # 11 workers with few tokens each, an odd layer: the gradient rows' bytes count
         gradient("gradient_n11_1000x1001x500", 11, 1000, 1001, 500, "float32"),
         # 19 workers' large batches: each worker's product into its row
@@ -95,8 +96,9 @@ def draw(rng):
     if rng.random() < 0.5:
         outputs, inputs = max(64, outputs // 64 * 64), max(64, inputs // 64 * 64)
     if kind == "linear":
+        out = rng.choice(["bfloat16", "float16", "float32"])
         return dict(kind=kind, tokens=_log(rng, 1, 16384), outputs=outputs, inputs=inputs,
-                    dtype=dtype, out=rng.choice(["bfloat16", "float16", "float32"]),
+                    dtype=dtype, out=out, fast=out != "float32" and rng.random() < 0.5,
                     bias=rng.random() < 0.5)
     return dict(kind=kind, workers=rng.randint(1, 19), tokens=_log(rng, 32, 16384),
                 outputs=outputs, inputs=inputs, dtype=dtype)
@@ -222,7 +224,8 @@ def _calls(s):
         return [c.restore(s["x"].dtype), c.exponents]
     if kind == "linear":
         w8 = gf.Checkpoint(*s["w8"], case["inputs"])
-        return gf.linear8(gf.checkpoint(s["x"]), w8, s["bias"], TYPES[case["out"]])
+        return gf.linear8(gf.checkpoint(s["x"]), w8, s["bias"], TYPES[case["out"]],
+                          fast=case["fast"])
     n, k, g = case["outputs"], case["inputs"], s["grads"]
     gf.weight_gradient(s["dy"], gf.Checkpoint(*s["x8"], k), s["counts"],
                        out=g[:, :n * k].view(-1, n, k), dbias=g[:, n * k:])
