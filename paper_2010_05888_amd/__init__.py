@@ -26,6 +26,8 @@ __all__ = [
     "distance_engine", "gram_reference", "table_gram_reference", "stream_read", "set_kernel_timing", "kernel_timing", "RULES",
     "ATTACKS", "attack", "variance_stats", "delta", "variance_condition", "Segmented",
     "SegmentTable", "contract_step", "contract",
+    "Checkpoint", "checkpoint", "LayerNorm", "layernorm", "layernorm_backward", "linear8",
+    "weight_gradient",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -635,3 +637,7 @@ def kernel_timing() -> dict:
 
 def distance_engine(n: int, d: int) -> str:
     return {0: "none", 1: "direct", 2: "gram"}[load().garfield_tuning_distance_engine(n, d)]
+
+
+from .worker import (Checkpoint, LayerNorm, checkpoint, layernorm,  # noqa: E402
+                     layernorm_backward, linear8, weight_gradient)

@@ -20,7 +20,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgarfield.so")
 
 SOURCES = ["dist.hip", "ring_direct.hip", "select.hip", "aggregate.hip", "byzantine.hip", "segtable.hip",
-           "contract.hip", "garfield_api.cpp", "timing.cpp"]
+           "contract.hip", "garfield_api.cpp", "timing.cpp",
+           "layernorm.hip", "block8.hip", "linear8.hip", "weight_gradient.hip", "worker_api.cpp"]
 
 ARCH = "gfx950"
 FLAGS = [

@@ -1,0 +1,324 @@
+"""A worker's operators: what comes before the aggregation rules.
+
+The n workers' tokens lie one worker after the other in a T x D matrix, and each
+worker's own weight gradient goes to its row of the n x d fp32 matrix that the
+rules take:
+
+    r = layernorm(x, weight, bias, y8=True, x8=True)       # y8: the linear layer's input,
+    out = linear8(r.y8, checkpoint(w), b, fast=True)       # kept in 8 bits with x8
+    ...                                                    # dout: the gradient of out
+    weight_gradient(dout, r.y8, counts, out=grads[:, i:j].view(n, *w.shape), dbias=...)
+    dy = linear8(checkpoint(dout), checkpoint(w, transposed=True), fast=True)
+    dx, _, _ = layernorm_backward(dy, r.x8, r.mean, r.rstd, weight, counts, dweight=..., dbias=...)
+    aggregate, sel = gar("multikrum", grads, f)
+
+Thin binding over the C-ABI of ``include/garfield_worker.h``, whose kernels do
+all the computing; calls run on the current stream of their tensors' device and
+share no scratch, so calls on several streams may overlap.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple
+
+import torch
+
+from . import GarfieldError, OK, load
+
+BLOCK = 128  # GARFIELD_BLOCK: values that share one exponent
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+_c = ctypes
+
+
+class _Block8(_c.Structure):
+    _fields_ = [("values", _c.c_void_p), ("exponents", _c.c_void_p), ("rows", _c.c_int64),
+                ("cols", _c.c_int64), ("ld_values", _c.c_int64), ("ld_exponents", _c.c_int64)]
+
+
+_vp, _i32, _i64, _sz, _f32 = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_size_t, _c.c_float
+_b8 = _c.POINTER(_Block8)
+_counts_p = _c.POINTER(_i64)
+_SIGNATURES = {
+    "garfield_checkpoint": (_i32, [_vp, _i32, _i64, _i64, _i64, _i32, _b8, _vp]),
+    "garfield_restore": (_i32, [_b8, _vp, _i32, _i64, _vp]),
+    "garfield_layernorm": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _i32, _f32, _vp, _i64,
+                                  _vp, _vp, _b8, _b8, _vp]),
+    "garfield_layernorm_backward_workspace": (_sz, [_i64, _i64, _i32, _counts_p]),
+    "garfield_layernorm_backward": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _b8, _vp, _vp,
+                                           _vp, _i32, _vp, _i64, _i32, _counts_p, _vp, _i64, _vp,
+                                           _i64, _vp, _sz, _vp]),
+    "garfield_linear8_workspace": (_sz, [_i64, _i64, _i64]),
+    "garfield_linear8": (_i32, [_b8, _b8, _vp, _i32, _vp, _i32, _i64, _vp, _sz, _vp]),
+    "garfield_weight_gradient_workspace": (_sz, [_i32, _i64, _i64, _i64, _i64, _i32, _counts_p]),
+    "garfield_weight_gradient": (_i32, [_vp, _i32, _i64, _i64, _i64, _b8, _i32, _counts_p, _vp,
+                                        _i64, _vp, _i64, _vp, _sz, _vp]),
+}
+_fn = {}
+
+
+def _functions():
+    if not _fn:
+        lib = load()
+        for name, (restype, argtypes) in _SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = restype, argtypes
+            _fn[name] = fn
+    return _fn
+
+
+def _run(name: str, device: torch.device, *args):
+    """Call a function of the library on the device's current stream."""
+    fn = _fn[name] if _fn else _functions()[name]
+    i = device.index
+    if i == torch.cuda.current_device():
+        code = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(i):
+            code = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    if code != OK:
+        raise GarfieldError(code, name, load().garfield_strerror(code).decode())
+
+
+def _matrix(x, name: str, dtype=None) -> torch.Tensor:
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor (one row a token)")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be on a GPU: this library has no CPU path")
+    if x.dtype not in TYPES or (dtype is not None and x.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype or 'float32, bfloat16 or float16'}")
+    if x.stride(1) != 1 and x.shape[1] > 1:
+        raise ValueError(f"{name}'s columns must be next to each other")
+    if x.stride(0) < x.shape[1] and x.shape[0] > 1:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return x
+
+
+def _ld(x: torch.Tensor) -> int:
+    return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], 1)
+
+
+def _vector(v, name: str, length: int, dtypes, device) -> torch.Tensor:
+    if (not isinstance(v, torch.Tensor) or v.dim() != 1 or v.shape[0] != length
+            or v.dtype not in dtypes or v.device != device or not v.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous 1-D tensor of {length} values of "
+                         f"{' or '.join(str(d) for d in dtypes)} on {device}")
+    return v
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _padded(cols: int):
+    """Columns of the codes and of the exponents that rows of cols values take."""
+    blocks = -(-cols // BLOCK)
+    return blocks * BLOCK, -(-blocks // 4) * 4
+
+
+class Checkpoint:
+    """A matrix of rows x cols values in 8-bit blocks (garfield_block8): codes
+    ``values`` (float8_e4m3fn, rows x the columns padded with zeros to a multiple
+    of 128) and ``exponents`` (uint8, one for each 128 values of a row, padded
+    with 127 to a multiple of four): the value of a code is code * 2^(exponent -
+    127). Made by ``checkpoint()`` and ``layernorm()``, or from tensors that hold
+    such blocks."""
+
+    __slots__ = ("values", "exponents", "rows", "cols", "device", "_held")
+
+    def __init__(self, values: torch.Tensor, exponents: torch.Tensor, cols: int):
+        if (not isinstance(values, torch.Tensor) or values.dim() != 2
+                or values.dtype != torch.float8_e4m3fn or not values.is_cuda):
+            raise ValueError("values must be a 2-D float8_e4m3fn tensor on a GPU")
+        if (not isinstance(exponents, torch.Tensor) or exponents.dim() != 2
+                or exponents.dtype != torch.uint8 or exponents.device != values.device):
+            raise ValueError("exponents must be a 2-D uint8 tensor on values' device")
+        width, held = _padded(cols)
+        rows = values.shape[0]
+        if values.shape[1] < width or exponents.shape[0] != rows or exponents.shape[1] < held:
+            raise ValueError(f"{cols} columns need {width} codes and {held} exponents a row")
+        ldv, lde = values.stride(0), exponents.stride(0)
+        if rows < 2:
+            ldv, lde = width, held
+        if cols > 0 and rows > 0 and (
+                values.stride(1) != 1 or exponents.stride(1) != 1 or ldv < width or ldv % 16
+                or lde < held or lde % 4 or values.data_ptr() % 16 or exponents.data_ptr() % 4):
+            raise ValueError("rows of codes must start at multiples of 16 bytes, rows of exponents "
+                             "at multiples of 4, their columns next to each other")
+        self._set(values, exponents, rows, cols, ldv, lde)
+
+    def _set(self, values, exponents, rows, cols, ldv, lde):
+        self.values, self.exponents, self.rows, self.cols = values, exponents, rows, cols
+        self.device = values.device
+        self._held = _Block8(values.data_ptr(), exponents.data_ptr(), rows, cols, ldv, lde)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device) -> "Checkpoint":
+        """Room for rows x cols values, to be written."""
+        width, held = _padded(cols)
+        c = cls.__new__(cls)
+        c._set(torch.empty((rows, width), dtype=torch.float8_e4m3fn, device=device),
+               torch.empty((rows, held), dtype=torch.uint8, device=device), rows, cols, width, held)
+        return c
+
+    def restore(self, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """The values, rounded once to dtype (bfloat16 and float32 hold them exactly)."""
+        if dtype not in TYPES:
+            raise ValueError("dtype must be float32, bfloat16 or float16")
+        out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.device)
+        _run("garfield_restore", self.device, self._held, out.data_ptr(), TYPES[dtype],
+             max(self.cols, 1))
+        return out
+
+
+def checkpoint(x: torch.Tensor, transposed: bool = False) -> Checkpoint:
+    """x (or its transpose) in 8-bit blocks of 128 values along a row of the result."""
+    x = _matrix(x, "x")
+    rows, cols = x.shape
+    c = Checkpoint.empty(*((cols, rows) if transposed else (rows, cols)), x.device)
+    _run("garfield_checkpoint", x.device, x.data_ptr(), TYPES[x.dtype], rows, cols, _ld(x),
+         int(transposed), c._held)
+    return c
+
+
+class LayerNorm(NamedTuple):
+    """What layernorm() gives: y (or None), each row's mean and 1 / deviation
+    (fp32), and the checkpoints of y and of x that were asked for (or None)."""
+    y: torch.Tensor | None
+    mean: torch.Tensor
+    rstd: torch.Tensor
+    y8: Checkpoint | None
+    x8: Checkpoint | None
+
+
+def _weights(x, weight, bias):
+    kinds = (torch.float32,) if x.dtype == torch.float32 else (torch.float32, x.dtype)
+    weight = _vector(weight, "weight", x.shape[1], kinds, x.device)
+    if bias is not None:
+        bias = _vector(bias, "bias", x.shape[1], (weight.dtype,), x.device)
+    return weight, bias
+
+
+def layernorm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None,
+              eps: float = 1e-5, y: bool = True, y8: bool = False,
+              x8: bool = False) -> LayerNorm:
+    """Layer norm of each row of x: (x - mean) * rstd * weight + bias in x's type
+    (y) and in 8-bit blocks (y8), and x itself in 8-bit blocks (x8)."""
+    x = _matrix(x, "x")
+    weight, bias = _weights(x, weight, bias)
+    rows, cols = x.shape
+    out = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if y else None
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    mean, rstd = stats[0], stats[1]
+    cy = Checkpoint.empty(rows, cols, x.device) if y8 else None
+    cx = Checkpoint.empty(rows, cols, x.device) if x8 else None
+    _run("garfield_layernorm", x.device, x.data_ptr(), TYPES[x.dtype], rows, cols, _ld(x),
+         weight.data_ptr(), _ptr(bias), TYPES[weight.dtype], eps, _ptr(out), max(cols, 1),
+         mean.data_ptr(), rstd.data_ptr(), cy._held if y8 else None, cx._held if x8 else None)
+    return LayerNorm(out, mean, rstd, cy, cx)
+
+
+def _counted(counts, rows: int):
+    """The workers' tokens as a C array (None: one worker)."""
+    counts = [rows] if counts is None else list(counts)
+    if not counts or sum(counts) != rows or min(counts) < 0:
+        raise ValueError(f"counts must be the workers' tokens, adding up to {rows}")
+    return len(counts), (_i64 * len(counts))(*counts)
+
+
+def _rows_of_workers(out, name: str, shape, device):
+    """The caller's rows of the gradients, or new ones; and their distance."""
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=device)
+    length = 1
+    for s in shape[1:]:
+        length *= s
+    inner = out[0] if isinstance(out, torch.Tensor) and out.dim() == len(shape) and shape[0] else None
+    if (inner is None or tuple(out.shape) != tuple(shape) or out.dtype != torch.float32
+            or out.device != device or not inner.is_contiguous()
+            or (shape[0] > 1 and out.stride(0) < length)):
+        raise ValueError(f"{name} must be a float32 tensor of {tuple(shape)} on {device}, each "
+                         "worker's values next to each other")
+    return out, out.stride(0) if shape[0] > 1 else length
+
+
+def _workspace(name: str, device, *args):
+    need = (_fn[name] if _fn else _functions()[name])(*args)
+    return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+
+
+def layernorm_backward(dy: torch.Tensor, x, mean: torch.Tensor, rstd: torch.Tensor,
+                       weight: torch.Tensor, counts=None, dweight: torch.Tensor | None = None,
+                       dbias: torch.Tensor | None = None):
+    """(dx, dweight, dbias) of layernorm(): x is its input, as a tensor of dy's
+    type or as a Checkpoint; counts the tokens of each of the n workers (None: one
+    worker). dweight and dbias (n x cols, float32) may be given, e.g. columns of
+    the matrix of gradients."""
+    dy = _matrix(dy, "dy")
+    rows, cols = dy.shape
+    dev = dy.device
+    x8 = x if isinstance(x, Checkpoint) else None
+    if x8 is None:
+        x = _matrix(x, "x", dy.dtype)
+    if (tuple((x8.rows, x8.cols) if x8 is not None else x.shape) != (rows, cols)
+            or x.device != dev):
+        raise ValueError("x must have dy's shape and device")
+    mean = _vector(mean, "mean", rows, (torch.float32,), dev)
+    rstd = _vector(rstd, "rstd", rows, (torch.float32,), dev)
+    weight, _ = _weights(dy, weight, None)
+    n, c = _counted(counts, rows)
+    dweight, ldw = _rows_of_workers(dweight, "dweight", (n, cols), dev)
+    dbias, ldb = _rows_of_workers(dbias, "dbias", (n, cols), dev)
+    dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
+    ws, need = _workspace("garfield_layernorm_backward_workspace", dev, rows, cols, n, c)
+    _run("garfield_layernorm_backward", dev, dy.data_ptr(), TYPES[dy.dtype], rows, cols, _ld(dy),
+         None if x8 is not None else x.data_ptr(), 0 if x8 is not None else _ld(x),
+         None if x8 is None else x8._held, mean.data_ptr(), rstd.data_ptr(), weight.data_ptr(),
+         TYPES[weight.dtype], dx.data_ptr(), max(cols, 1), n, c, dweight.data_ptr(), ldw,
+         dbias.data_ptr(), ldb, _ptr(ws), need)
+    return dx, dweight, dbias
+
+
+def linear8(x8: Checkpoint, w8: Checkpoint, bias: torch.Tensor | None = None,
+            dtype: torch.dtype = torch.bfloat16, fast: bool = False) -> torch.Tensor:
+    """x w^T + bias of two checkpoints (rows of x by rows of w), in dtype; bias is
+    float32. Sums are fp32; with fast they may be the 8-bit matrix instruction's,
+    which runs at twice the rate and keeps 14 bits of every eight products."""
+    if not isinstance(x8, Checkpoint) or not isinstance(w8, Checkpoint):
+        raise ValueError("x8 and w8 must be checkpoints")
+    if x8.cols != w8.cols or x8.device != w8.device:
+        raise ValueError("x8 and w8 must have the same columns and device")
+    if dtype not in TYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    if bias is not None:
+        bias = _vector(bias, "bias", w8.rows, (torch.float32,), x8.device)
+    out = torch.empty((x8.rows, w8.rows), dtype=dtype, device=x8.device)
+    ws, need = _workspace("garfield_linear8_workspace", x8.device, x8.rows, w8.rows, x8.cols)
+    _run("garfield_linear8", x8.device, x8._held, w8._held, _ptr(bias), int(fast), out.data_ptr(),
+         TYPES[dtype], max(w8.rows, 1), _ptr(ws), need)
+    return out
+
+
+def weight_gradient(dy: torch.Tensor, x8: Checkpoint, counts=None,
+                    out: torch.Tensor | None = None, dbias: torch.Tensor | None = None):
+    """(dw, dbias) of a linear layer for each worker: dw[w] = dy^T x over worker
+    w's tokens (n x outputs x inputs, float32) and dbias[w] = their sum of dy. dy:
+    the gradient of the layer's output; x8: the checkpoint of its input; out and
+    dbias may be given, e.g. columns of the matrix of gradients (dbias is None
+    where it is not given)."""
+    dy = _matrix(dy, "dy")
+    tokens, outputs = dy.shape
+    dev = dy.device
+    if not isinstance(x8, Checkpoint) or x8.rows != tokens or x8.device != dev:
+        raise ValueError("x8 must be a checkpoint with dy's rows and device")
+    n, c = _counted(counts, tokens)
+    out, ld = _rows_of_workers(out, "out", (n, outputs, x8.cols), dev)
+    ldb = outputs
+    if dbias is not None:
+        dbias, ldb = _rows_of_workers(dbias, "dbias", (n, outputs), dev)
+    kind = TYPES[dy.dtype]
+    ws, need = _workspace("garfield_weight_gradient_workspace", dev, kind, tokens, outputs, x8.cols,
+                          _ld(dy), n, c)
+    _run("garfield_weight_gradient", dev, dy.data_ptr(), kind, tokens, outputs, _ld(dy), x8._held,
+         n, c, out.data_ptr(), ld, _ptr(dbias), ldb, _ptr(ws), need)
+    return out, dbias
