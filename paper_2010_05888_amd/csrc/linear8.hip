@@ -22,44 +22,18 @@ namespace garfield {
 
 namespace {
 
-__device__ __forceinline__ i8v load32(const uint8_t* p) {
-  union {
-    u4 h[2];
-    i8v v;
-  } t;
-  t.h[0] = reinterpret_cast<const u4*>(p)[0];
-  t.h[1] = reinterpret_cast<const u4*>(p)[1];
-  return t.v;
-}
-
 // Eight codes of a lane as bf16 values.
-__device__ __forceinline__ bf8 decode_bf16(uint32_t lo, uint32_t hi, float scale) {
+__device__ __forceinline__ bf8 decode_bf16(u2 q, float scale) {
   typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
   union {
     bf2 h[4];
     bf8 v;
   } t;
-  t.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-  t.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  t.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-  t.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  t.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.x, scale, false);
+  t.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.x, scale, true);
+  t.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.y, scale, false);
+  t.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.y, scale, true);
   return t.v;
-}
-
-// c + a b over a block; sa and sb are the exponents as they are stored.
-template <bool FAST>
-__device__ __forceinline__ v4f product(i8v a, i8v b, v4f c, int sa, int sb) {
-  if constexpr (FAST) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
-  } else {
-    const float fa = power2(sa - 127), fb = power2(sb - 127);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode_bf16(a[2 * i], a[2 * i + 1], fa),
-                                                  decode_bf16(b[2 * i], b[2 * i + 1], fb), c, 0, 0,
-                                                  0);
-    return c;
-  }
 }
 
 // Four outputs of one token (fewer at the row's end).
@@ -79,55 +53,196 @@ __device__ __forceinline__ void store_outputs(T* out, const float* bias, int64_t
   }
 }
 
-// A wave takes 16 outputs of 64 tokens, operands straight from memory.
-template <typename T, bool FAST>
-__global__ __launch_bounds__(kBlock) void k_linear8(garfield_block8 x, garfield_block8 w,
-                                                    const float* __restrict__ bias, T* out,
-                                                    int64_t ld, uint32_t across) {
+typedef __attribute__((address_space(1))) const void* GlobalPtr;
+typedef __attribute__((address_space(3))) void* LocalPtr;
+
+// Workgroup id to tile: workgroups go to the eight XCDs in turn, so an XCD's
+// share is made contiguous, and inside it eight token tiles deep: the tiles that
+// an XCD has in work share their rows of X and W in its L2.
+struct Place {
+  int64_t m, j;
+};
+__device__ __forceinline__ Place place_of(uint32_t id, uint32_t total, uint32_t tiles_m,
+                                          uint32_t tiles_j) {
+  constexpr uint32_t kXcds = 8, kDeep = 8;
+  const uint32_t share = total / kXcds, more = total % kXcds, xcd = id % kXcds;
+  const uint32_t at = xcd * share + (xcd < more ? xcd : more) + id / kXcds;
+  const uint32_t group = kDeep * tiles_j, first = at / group * kDeep;
+  const uint32_t deep = tiles_m - first < kDeep ? tiles_m - first : kDeep;
+  return {first + at % group % deep, at % group / deep};
+}
+
+// A workgroup makes a tile of WJ * FA * 16 outputs x WM * FB * 16 tokens, a wave
+// FA x FB products of 16 x 16, block after block of 128 columns. The next
+// block's codes go from memory straight to LDS while the waves work on this one,
+// the exponents of four blocks with every fourth of them.
+// A row of 128 codes is eight 16-byte chunks, chunk c at c ^ (row % 8), so that the
+// rows that a wave reads together lie in different banks. Lane l takes chunks
+// 2 (l / 16) and 2 (l / 16) + 1 of its rows.
+// Offset: of a row from its tile's first one.
+template <typename T, bool FAST, typename Offset, int WJ, int WM, int FA, int FB>
+__global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
+    garfield_block8 x, garfield_block8 w, const float* __restrict__ bias, T* out, int64_t ld,
+    uint32_t tiles_m, uint32_t tiles_j) {
+  constexpr int kWaves = WJ * WM, kTileJ = WJ * FA * 16, kTileM = WM * FB * 16;
+  constexpr int kRows = kTileJ + kTileM, kLoads = kRows / 8 / kWaves;  // eight rows a load
+  static_assert(kRows % (8 * kWaves) == 0 && kTileJ % 64 == 0 && kTileM % 64 == 0,
+                "rows are shared out evenly");
+  static_assert(kRows <= 64 * kWaves, "a wave fetches the exponents of 64 rows");
+  // codes of two blocks, exponents of two groups of four
+  constexpr int kCodes = kRows * kBlock8, kExponents = kRows * 4;
+  __shared__ __align__(1024) uint8_t lds[2 * (kCodes + kExponents)];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t j0 = (static_cast<int64_t>(blockIdx.x % across) * 4 + wave) * 16;
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x / across) * 64;
-  if (j0 >= w.rows) return;
-  const int64_t j = j0 + lane % 16 < w.rows ? j0 + lane % 16 : w.rows - 1;
-  const uint8_t* wv = w.values + j * w.ld_values + lane / 16 * 32;
-  const uint8_t* we = w.exponents + j * w.ld_exponents;
-  const uint8_t *xv[4], *xe[4];
-  v4f sum[4];
+  const Place at = place_of(blockIdx.x, gridDim.x, tiles_m, tiles_j);
+  const int64_t j0 = at.j * kTileJ, m0 = at.m * kTileM;
+
+  // rows of the tile: W's, then X's; those past the end read the last one again
+  const int left_j = static_cast<int>(w.rows - j0 < kTileJ ? w.rows - j0 : kTileJ) - 1;
+  const int left_m = static_cast<int>(x.rows - m0 < kTileM ? x.rows - m0 : kTileM) - 1;
+  const uint8_t* const w0 = w.values + j0 * w.ld_values;
+  const uint8_t* const x0 = x.values + m0 * x.ld_values;
+  Offset from[kLoads];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    int64_t m = m0 + 16 * i + lane % 16;
-    m = m < x.rows ? m : x.rows - 1;
-    xv[i] = x.values + m * x.ld_values + lane / 16 * 32;
-    xe[i] = x.exponents + m * x.ld_exponents;
-    sum[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < kLoads; ++i) {
+    const bool of_w = i < kLoads * kTileJ / kRows;
+    int row = (i * kWaves + wave) * 8 + lane / 8 - (of_w ? 0 : kTileJ);
+    const int last = of_w ? left_j : left_m;
+    row = row < last ? row : last;
+    from[i] = static_cast<Offset>(row) * static_cast<Offset>(of_w ? w.ld_values : x.ld_values) +
+              ((lane % 8) ^ (lane / 8)) * 16;
   }
-  const int64_t blocks = (x.cols + kBlock8 - 1) / kBlock8;
-  for (int64_t b = 0; b < blocks; ++b) {
-    const i8v a = load32(wv + b * kBlock8);
-    const int sa = we[b];
+  static_assert(kLoads * kTileJ % kRows == 0, "a load is of W's rows or of X's");
+  const uint8_t* e0;
+  {
+    int row = wave * 64 + lane;
+    const bool of_w = row < kTileJ;
+    row -= of_w ? 0 : kTileJ;
+    const int last = of_w ? left_j : left_m;
+    row = row < last ? row : last;
+    e0 = of_w ? w.exponents + (j0 + row) * w.ld_exponents
+              : x.exponents + (m0 + row) * x.ld_exponents;
+  }
+  auto fetch = [&](int block) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = product<FAST>(a, load32(xv[i] + b * kBlock8), sum[i], sa, xe[i][b]);
+    for (int i = 0; i < kLoads; ++i) {
+      const uint8_t* base = (i < kLoads * kTileJ / kRows ? w0 : x0) + block * int64_t{kBlock8};
+      __builtin_amdgcn_global_load_lds((GlobalPtr)(base + from[i]),
+                                       (LocalPtr)(lds + (block & 1) * kCodes + (i * kWaves + wave) * 1024),
+                                       16, 0, 0);
+    }
+    if (block % 4 == 0 && wave * 64 < kRows)
+      __builtin_amdgcn_global_load_lds((GlobalPtr)(e0 + block),
+                                       (LocalPtr)(lds + 2 * kCodes + (block / 4 & 1) * kExponents +
+                                                  wave * 256),
+                                       4, 0, 0);
+  };
+
+  const int wj = wave / WM, wm = wave % WM;
+  v4f sum[FA][FB];
+#pragma unroll
+  for (int i = 0; i < FA; ++i)
+#pragma unroll
+    for (int k = 0; k < FB; ++k) sum[i][k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int blocks = static_cast<int>((x.cols + kBlock8 - 1) / kBlock8);
+  const int row0 = lane % 16 * kBlock8, chunk0 = (lane / 16 * 2) ^ (lane % 8);
+  const int near0 = row0 + chunk0 * 16, near1 = row0 + (chunk0 ^ 1) * 16;
+  uint32_t ew[FA], ex[FB];
+  if (blocks > 0) fetch(0);
+  for (int b = 0; b < blocks; ++b) {
+    __syncthreads();  // block b is there, and block b - 1 has been read
+    if (b + 1 < blocks) fetch(b + 1);
+    if (b % 4 == 0) {
+      const uint32_t* e = reinterpret_cast<const uint32_t*>(lds + 2 * kCodes +
+                                                            (b / 4 & 1) * kExponents) + lane % 16;
+#pragma unroll
+      for (int i = 0; i < FA; ++i) ew[i] = e[(wj * FA + i) * 16];
+#pragma unroll
+      for (int i = 0; i < FB; ++i) ex[i] = e[kTileJ + (wm * FB + i) * 16];
+    }
+    const uint8_t* wt = lds + (b & 1) * kCodes + wj * FA * 16 * kBlock8;
+    const uint8_t* xt = lds + (b & 1) * kCodes + (kTileJ + wm * FB * 16) * kBlock8;
+    const int by = b % 4 * 8;
+    if constexpr (FAST) {
+      auto read = [&](const uint8_t* p) {
+        union {
+          u4 h[2];
+          i8v v;
+        } t;
+        t.h[0] = *reinterpret_cast<const u4*>(p + near0);
+        t.h[1] = *reinterpret_cast<const u4*>(p + near1);
+        return t.v;
+      };
+      i8v xf[FB], wf[2];
+#pragma unroll
+      for (int k = 0; k < FB; ++k) xf[k] = read(xt + k * 16 * kBlock8);
+      wf[0] = read(wt);
+#pragma unroll
+      for (int i = 0; i < FA; ++i) {
+        if (i + 1 < FA) wf[(i + 1) & 1] = read(wt + (i + 1) * 16 * kBlock8);
+#pragma unroll
+        for (int k = 0; k < FB; ++k)
+          sum[i][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              wf[i & 1], xf[k], sum[i][k], 0, 0, 0, ew[i] >> by & 255, 0, ex[k] >> by & 255);
+      }
+    } else {
+      // a quarter of the lane's codes at a time
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int near = (q < 2 ? near0 : near1) + q % 2 * 8;
+        bf8 xf[FB];
+#pragma unroll
+        for (int k = 0; k < FB; ++k)
+          xf[k] = decode_bf16(*reinterpret_cast<const u2*>(xt + k * 16 * kBlock8 + near),
+                              __uint_as_float((ex[k] >> by & 255) << 23));
+#pragma unroll
+        for (int i = 0; i < FA; ++i) {
+          const bf8 wf = decode_bf16(*reinterpret_cast<const u2*>(wt + i * 16 * kBlock8 + near),
+                                     __uint_as_float((ew[i] >> by & 255) << 23));
+#pragma unroll
+          for (int k = 0; k < FB; ++k)
+            sum[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[k], sum[i][k], 0, 0, 0);
+        }
+      }
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t m = m0 + 16 * i + lane % 16;
-    if (m < x.rows) store_outputs(out + m * ld, bias, j0 + lane / 16 * 4, w.rows, sum[i]);
+  for (int k = 0; k < FB; ++k) {
+    const int64_t m = m0 + (wm * FB + k) * 16 + lane % 16;
+    if (m >= x.rows) continue;
+#pragma unroll
+    for (int i = 0; i < FA; ++i)
+      store_outputs(out + m * ld, bias, j0 + (wj * FA + i) * 16 + lane / 16 * 4, w.rows,
+                    sum[i][k]);
   }
 }
 
+template <typename T, bool FAST, typename Offset, int WJ, int WM, int FA, int FB>
+void launch_tile(const garfield_block8& x, const garfield_block8& w, const float* bias, void* out,
+                 int64_t ld, hipStream_t s) {
+  const uint32_t tiles_j = static_cast<uint32_t>((w.rows + WJ * FA * 16 - 1) / (WJ * FA * 16));
+  const uint32_t tiles_m = static_cast<uint32_t>((x.rows + WM * FB * 16 - 1) / (WM * FB * 16));
+  launch("linear8", k_linear8_tile<T, FAST, Offset, WJ, WM, FA, FB>, dim3(tiles_j * tiles_m),
+         dim3(64 * WJ * WM), 0, s, x, w, bias, static_cast<T*>(out), ld, tiles_m, tiles_j);
+}
+
 template <typename T, bool FAST>
-void launch_linear8(const garfield_block8& x, const garfield_block8& w, const float* bias,
-                    void* out, int64_t ld, hipStream_t s) {
-  const uint32_t across = static_cast<uint32_t>((w.rows + 63) / 64);
-  launch("linear8", k_linear8<T, FAST>, dim3(across * static_cast<uint32_t>((x.rows + 63) / 64)),
-         dim3(kBlock), 0, s, x, w, bias, static_cast<T*>(out), ld, across);
+void choose_tile(const garfield_block8& x, const garfield_block8& w, const float* bias, void* out,
+                 int64_t ld, hipStream_t s) {
+  const int64_t large = ((w.rows + 255) / 256) * ((x.rows + 255) / 256);
+  const int64_t middle = ((w.rows + 127) / 128) * ((x.rows + 127) / 128);
+  if (x.ld_values > 0xffffff || w.ld_values > 0xffffff)  // 256 rows pass 32 bits
+    launch_tile<T, FAST, int64_t, 2, 2, 2, 2>(x, w, bias, out, ld, s);
+  else if (large >= 192) launch_tile<T, FAST, uint32_t, 2, 4, 8, 4>(x, w, bias, out, ld, s);
+  else if (middle >= 192) launch_tile<T, FAST, uint32_t, 2, 2, 4, 4>(x, w, bias, out, ld, s);
+  else launch_tile<T, FAST, uint32_t, 2, 2, 2, 2>(x, w, bias, out, ld, s);
 }
 
 template <typename T>
 void choose_linear8(const garfield_block8& x, const garfield_block8& w, const float* bias,
                     bool fast, void* out, int64_t ld, hipStream_t s) {
-  if (fast) launch_linear8<T, true>(x, w, bias, out, ld, s);
-  else launch_linear8<T, false>(x, w, bias, out, ld, s);
+  if (fast) choose_tile<T, true>(x, w, bias, out, ld, s);
+  else choose_tile<T, false>(x, w, bias, out, ld, s);
 }
 
 }  // namespace
