@@ -19,6 +19,8 @@
  *     enqueues kernels only, so it can be captured in a graph.
  *   - Sizes of zero are allowed (sums over nothing are 0), except the columns
  *     of a layer norm.
+ *   - A matrix has at most 2^25 rows, 2^30 columns and 2^34 values (its columns
+ *     rounded up to 512); GARFIELD_ETOOBIG beyond.
  *   - Infinities and NaN are allowed and stay where they come from: a row of
  *     a layer norm, a token of a product, a worker's gradient. Another row,
  *     token or worker never sees them.
@@ -138,10 +140,11 @@ garfield_status garfield_linear8(const garfield_block8* x, const garfield_block8
  *   dbias[w][j] = sum_t dy[t][j]          (dbias may be NULL).
  * Every product is exact (dy of more bits than bf16 is split into bf16 parts,
  * two of fp16 and three of fp32: fp32 values below about 2^-110 may lose their
- * last parts), sums are fp32.
+ * last parts), sums are fp32. At most 2^24 outputs, rows of x at most 2^26 bytes
+ * apart (GARFIELD_ETOOBIG beyond).
  */
-size_t garfield_weight_gradient_workspace(int type, int64_t tokens, int64_t outputs,
-                                          int64_t inputs, int64_t lddy, int n,
+size_t garfield_weight_gradient_workspace(const void* dy, int type, int64_t tokens,
+                                          int64_t outputs, int64_t inputs, int64_t lddy, int n,
                                           const int64_t* counts);
 garfield_status garfield_weight_gradient(const void* dy, int type, int64_t tokens,
                                          int64_t outputs, int64_t lddy, const garfield_block8* x,

@@ -75,7 +75,7 @@ struct WeightGradient {
   int64_t ld_dbias;
 };
 size_t weight_gradient_bytes(int type, int64_t tokens, int64_t outputs, int64_t inputs,
-                             int64_t lddy, int n, const int64_t* counts);
+                             const void* dy, int64_t lddy, int n, const int64_t* counts);
 hipError_t enqueue_weight_gradient(const WeightGradient& a, void* workspace, hipStream_t s);
 
 }  // namespace garfield

@@ -10,11 +10,14 @@
 namespace garfield {
 namespace {
 
-// Beyond these a launch's grid or an index into a row would not hold. Offsets
-// into a matrix are 64-bit.
-constexpr int64_t kMaxRows = int64_t{1} << 30;
+// Beyond these a launch would have more than 2^32 threads, or an index into a
+// row would not fit. Offsets into a matrix are 64-bit.
+constexpr int64_t kMaxRows = int64_t{1} << 25;
 constexpr int64_t kMaxCols = int64_t{1} << 30;
-constexpr int64_t kMaxBlocks = int64_t{1} << 33;  // of one matrix
+constexpr int64_t kMaxBlocks = int64_t{1} << 27;  // of one matrix, padded
+// Weight gradients address 32 tokens with 32 bits.
+constexpr int64_t kMaxOutputs = int64_t{1} << 24;
+constexpr int64_t kMaxStride = int64_t{1} << 26;
 
 garfield_status status_of(hipError_t e) {
   if (e == hipSuccess) return GARFIELD_OK;
@@ -215,14 +218,14 @@ garfield_status garfield_linear8(const garfield_block8* x, const garfield_block8
                                    static_cast<hipStream_t>(stream)));
 }
 
-size_t garfield_weight_gradient_workspace(int type, int64_t tokens, int64_t outputs,
-                                          int64_t inputs, int64_t lddy, int n,
+size_t garfield_weight_gradient_workspace(const void* dy, int type, int64_t tokens,
+                                          int64_t outputs, int64_t inputs, int64_t lddy, int n,
                                           const int64_t* counts) {
   if (!is_type(type) || check_size(tokens, inputs) != GARFIELD_OK ||
       check_size(tokens, outputs) != GARFIELD_OK || check_size(outputs, inputs) != GARFIELD_OK ||
       check_counts(n, counts, tokens) != GARFIELD_OK)
     return 0;
-  return weight_gradient_bytes(type, tokens, outputs, inputs, lddy, n, counts);
+  return weight_gradient_bytes(type, tokens, outputs, inputs, dy, lddy, n, counts);
 }
 
 garfield_status garfield_weight_gradient(const void* dy, int type, int64_t tokens,
@@ -236,13 +239,15 @@ garfield_status garfield_weight_gradient(const void* dy, int type, int64_t token
   if (st == GARFIELD_OK) st = check_size(outputs, x->cols);
   if (st == GARFIELD_OK) st = check_counts(n, counts, tokens);
   if (st != GARFIELD_OK) return st;
+  if (outputs > kMaxOutputs || x->ld_values > kMaxStride || x->ld_exponents > kMaxStride)
+    return GARFIELD_ETOOBIG;
   const int64_t length = outputs * x->cols;
   if (!matrix_ok(dy, type, tokens, outputs, lddy) || !block8_ok(x, tokens, x->cols) ||
       (length > 0 && !dw) || !gradient_ok(dw, n, length, ld_dw) ||
       !gradient_ok(dbias, n, outputs, ld_dbias))
     return GARFIELD_EINVAL;
   if (!workspace_ok(workspace, workspace_bytes,
-                    weight_gradient_bytes(type, tokens, outputs, x->cols, lddy, n, counts)))
+                    weight_gradient_bytes(type, tokens, outputs, x->cols, dy, lddy, n, counts)))
     return GARFIELD_EINVAL;
   if (outputs == 0) return GARFIELD_OK;
   WeightGradient a = {};

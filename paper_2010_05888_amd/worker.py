@@ -50,7 +50,8 @@ _SIGNATURES = {
                                            _i64, _vp, _sz, _vp]),
     "garfield_linear8_workspace": (_sz, [_i64, _i64, _i64]),
     "garfield_linear8": (_i32, [_b8, _b8, _vp, _i32, _vp, _i32, _i64, _vp, _sz, _vp]),
-    "garfield_weight_gradient_workspace": (_sz, [_i32, _i64, _i64, _i64, _i64, _i32, _counts_p]),
+    "garfield_weight_gradient_workspace": (_sz, [_vp, _i32, _i64, _i64, _i64, _i64, _i32,
+                                                 _counts_p]),
     "garfield_weight_gradient": (_i32, [_vp, _i32, _i64, _i64, _i64, _b8, _i32, _counts_p, _vp,
                                         _i64, _vp, _i64, _vp, _sz, _vp]),
 }
@@ -317,8 +318,8 @@ def weight_gradient(dy: torch.Tensor, x8: Checkpoint, counts=None,
     if dbias is not None:
         dbias, ldb = _rows_of_workers(dbias, "dbias", (n, outputs), dev)
     kind = TYPES[dy.dtype]
-    ws, need = _workspace("garfield_weight_gradient_workspace", dev, kind, tokens, outputs, x8.cols,
-                          _ld(dy), n, c)
+    ws, need = _workspace("garfield_weight_gradient_workspace", dev, dy.data_ptr(), kind, tokens,
+                          outputs, x8.cols, _ld(dy), n, c)
     _run("garfield_weight_gradient", dev, dy.data_ptr(), kind, tokens, outputs, _ld(dy), x8._held,
          n, c, out.data_ptr(), ld, _ptr(dbias), ldb, _ptr(ws), need)
     return out, dbias
