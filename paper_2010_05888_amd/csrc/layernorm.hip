@@ -206,10 +206,11 @@ __device__ __forceinline__ void load_x(const LayerNormBackward& a, int64_t row, 
   }
 }
 
+// The worker whose chunk it is: as many workers end at or before it.
 __device__ __forceinline__ int worker_of(const Chunks& c, int chunk) {
-  int w = 0;
-  while (c.chunk0[w + 1] <= chunk) ++w;
-  return w;
+  const int lane = threadIdx.x % 64;
+  static_assert(kWorkersMax == 64, "a lane looks at one worker");
+  return __builtin_popcountll(__ballot(lane < c.n && c.chunk0[lane + 1] <= chunk));
 }
 
 // A workgroup goes through one chunk of a worker's rows (up to 8 * THREADS * NV

@@ -53,6 +53,92 @@ __device__ __forceinline__ void store_outputs(T* out, const float* bias, int64_t
   }
 }
 
+// Few tokens (up to 16 * FB): the time is W's bytes. A workgroup takes 16 outputs,
+// its waves every WAVES-th block each, operands straight from memory and several
+// blocks at a time; the waves' sums meet in LDS, added in one order. Products are
+// bf16's: the matrix instructions are idle most of the time either way.
+template <typename T, int WAVES, int FB>
+__global__ __launch_bounds__(64 * WAVES) void k_linear8_few(garfield_block8 x, garfield_block8 w,
+                                                            const float* __restrict__ bias, T* out,
+                                                            int64_t ld) {
+  constexpr int kAtOnce = FB == 1 ? 4 : FB == 2 ? 2 : 1;
+  __shared__ v4f sums[WAVES][FB][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t j0 = static_cast<int64_t>(blockIdx.x) * 16;
+  const int64_t j = j0 + lane % 16 < w.rows ? j0 + lane % 16 : w.rows - 1;
+  const uint8_t* wv = w.values + j * w.ld_values + lane / 16 * 32;
+  const uint8_t* we = w.exponents + j * w.ld_exponents;
+  const uint8_t *xv[FB], *xe[FB];
+  v4f sum[FB];
+#pragma unroll
+  for (int k = 0; k < FB; ++k) {
+    const int64_t m = 16 * k + lane % 16 < x.rows ? 16 * k + lane % 16 : x.rows - 1;
+    xv[k] = x.values + m * x.ld_values + lane / 16 * 32;
+    xe[k] = x.exponents + m * x.ld_exponents;
+    sum[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  const int blocks = static_cast<int>((x.cols + kBlock8 - 1) / kBlock8);
+  for (int b0 = wave; b0 < blocks; b0 += WAVES * kAtOnce) {
+    u4 wc[kAtOnce][2], xc[kAtOnce][FB][2];
+    uint32_t ws[kAtOnce], xs[kAtOnce][FB];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int b = b0 + u * WAVES < blocks ? b0 + u * WAVES : blocks - 1;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        wc[u][h] = reinterpret_cast<const u4*>(wv + static_cast<int64_t>(b) * kBlock8)[h];
+      ws[u] = we[b];
+#pragma unroll
+      for (int k = 0; k < FB; ++k) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          xc[u][k][h] = reinterpret_cast<const u4*>(xv[k] + static_cast<int64_t>(b) * kBlock8)[h];
+        xs[u][k] = xe[k][b];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (b0 + u * WAVES >= blocks) break;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bf8 wf = decode_bf16(u2{wc[u][q / 2][q % 2 * 2], wc[u][q / 2][q % 2 * 2 + 1]},
+                                   __uint_as_float(ws[u] << 23));
+#pragma unroll
+        for (int k = 0; k < FB; ++k)
+          sum[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              wf,
+              decode_bf16(u2{xc[u][k][q / 2][q % 2 * 2], xc[u][k][q / 2][q % 2 * 2 + 1]},
+                          __uint_as_float(xs[u][k] << 23)),
+              sum[k], 0, 0, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < FB; ++k) sums[wave][k][lane] = sum[k];
+  __syncthreads();
+  if (wave >= FB) return;
+  v4f all = sums[0][wave][lane];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) all += sums[i][wave][lane];
+  const int64_t m = 16 * wave + lane % 16;
+  if (m < x.rows) store_outputs(out + m * ld, bias, j0 + lane / 16 * 4, w.rows, all);
+}
+
+template <typename T, int WAVES, int FB>
+void launch_few(const garfield_block8& x, const garfield_block8& w, const float* bias, void* out,
+                int64_t ld, hipStream_t s) {
+  launch("linear8_few", k_linear8_few<T, WAVES, FB>, dim3(static_cast<uint32_t>((w.rows + 15) / 16)),
+         dim3(64 * WAVES), 0, s, x, w, bias, static_cast<T*>(out), ld);
+}
+
+template <typename T, int FB>
+void choose_few(const garfield_block8& x, const garfield_block8& w, const float* bias, void* out,
+                int64_t ld, hipStream_t s) {
+  if (x.cols > 16 * kBlock8) launch_few<T, 16, FB>(x, w, bias, out, ld, s);
+  else if (x.cols > 4 * kBlock8) launch_few<T, 8, FB>(x, w, bias, out, ld, s);
+  else launch_few<T, 4, FB>(x, w, bias, out, ld, s);
+}
+
 typedef __attribute__((address_space(1))) const void* GlobalPtr;
 typedef __attribute__((address_space(3))) void* LocalPtr;
 
@@ -241,7 +327,10 @@ void choose_tile(const garfield_block8& x, const garfield_block8& w, const float
 template <typename T>
 void choose_linear8(const garfield_block8& x, const garfield_block8& w, const float* bias,
                     bool fast, void* out, int64_t ld, hipStream_t s) {
-  if (fast) choose_tile<T, true>(x, w, bias, out, ld, s);
+  if (x.rows <= 16) choose_few<T, 1>(x, w, bias, out, ld, s);
+  else if (x.rows <= 32) choose_few<T, 2>(x, w, bias, out, ld, s);
+  else if (x.rows <= 64) choose_few<T, 4>(x, w, bias, out, ld, s);
+  else if (fast) choose_tile<T, true>(x, w, bias, out, ld, s);
   else choose_tile<T, false>(x, w, bias, out, ld, s);
 }
 

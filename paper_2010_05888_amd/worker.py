@@ -70,9 +70,9 @@ def _functions():
 
 def _run(name: str, device: torch.device, *args):
     """Call a function of the library on the device's current stream."""
-    fn = _fn[name] if _fn else _functions()[name]
+    fn = _fn.get(name) or _functions()[name]
     i = device.index
-    if i == torch.cuda.current_device():
+    if i == torch._C._cuda_getDevice():
         code = fn(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(i):
@@ -81,34 +81,32 @@ def _run(name: str, device: torch.device, *args):
         raise GarfieldError(code, name, load().garfield_strerror(code).decode())
 
 
-def _matrix(x, name: str, dtype=None) -> torch.Tensor:
+def _matrix(x, name: str, dtype=None):
+    """x's rows, columns, row distance and type."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise ValueError(f"{name} must be a 2-D tensor (one row a token)")
     if not x.is_cuda:
         raise ValueError(f"{name} must be on a GPU: this library has no CPU path")
-    if x.dtype not in TYPES or (dtype is not None and x.dtype != dtype):
+    kind = TYPES.get(x.dtype)
+    if kind is None or (dtype is not None and x.dtype != dtype):
         raise ValueError(f"{name} must be {dtype or 'float32, bfloat16 or float16'}")
-    if x.stride(1) != 1 and x.shape[1] > 1:
+    rows, cols = x.shape
+    ld, step = x.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}'s columns must be next to each other")
-    if x.stride(0) < x.shape[1] and x.shape[0] > 1:
+    if rows < 2:
+        ld = cols or 1
+    elif ld < cols:
         raise ValueError(f"{name}'s rows must not overlap")
-    return x
+    return rows, cols, ld, kind
 
 
-def _ld(x: torch.Tensor) -> int:
-    return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], 1)
-
-
-def _vector(v, name: str, length: int, dtypes, device) -> torch.Tensor:
-    if (not isinstance(v, torch.Tensor) or v.dim() != 1 or v.shape[0] != length
-            or v.dtype not in dtypes or v.device != device or not v.is_contiguous()):
+def _vector(v, name: str, length: int, dtypes, device):
+    if (not isinstance(v, torch.Tensor) or v.shape != (length,) or v.dtype not in dtypes
+            or v.device != device or not v.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous 1-D tensor of {length} values of "
                          f"{' or '.join(str(d) for d in dtypes)} on {device}")
-    return v
-
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
+    return v.data_ptr()
 
 
 def _padded(cols: int):
@@ -125,7 +123,7 @@ class Checkpoint:
     127). Made by ``checkpoint()`` and ``layernorm()``, or from tensors that hold
     such blocks."""
 
-    __slots__ = ("values", "exponents", "rows", "cols", "device", "_held")
+    __slots__ = ("rows", "cols", "device", "_held", "_flat", "_values", "_exponents")
 
     def __init__(self, values: torch.Tensor, exponents: torch.Tensor, cols: int):
         if (not isinstance(values, torch.Tensor) or values.dim() != 2
@@ -135,32 +133,49 @@ class Checkpoint:
                 or exponents.dtype != torch.uint8 or exponents.device != values.device):
             raise ValueError("exponents must be a 2-D uint8 tensor on values' device")
         width, held = _padded(cols)
-        rows = values.shape[0]
-        if values.shape[1] < width or exponents.shape[0] != rows or exponents.shape[1] < held:
+        rows, codes = values.shape
+        rows_held, codes_held = exponents.shape
+        if codes < width or rows_held != rows or codes_held < held:
             raise ValueError(f"{cols} columns need {width} codes and {held} exponents a row")
-        ldv, lde = values.stride(0), exponents.stride(0)
+        (ldv, step), (lde, step_held) = values.stride(), exponents.stride()
         if rows < 2:
             ldv, lde = width, held
-        if cols > 0 and rows > 0 and (
-                values.stride(1) != 1 or exponents.stride(1) != 1 or ldv < width or ldv % 16
-                or lde < held or lde % 4 or values.data_ptr() % 16 or exponents.data_ptr() % 4):
+        pv, pe = values.data_ptr(), exponents.data_ptr()
+        if cols > 0 and rows > 0 and (step != 1 or step_held != 1 or ldv < width or ldv % 16
+                                      or lde < held or lde % 4 or pv % 16 or pe % 4):
             raise ValueError("rows of codes must start at multiples of 16 bytes, rows of exponents "
                              "at multiples of 4, their columns next to each other")
-        self._set(values, exponents, rows, cols, ldv, lde)
-
-    def _set(self, values, exponents, rows, cols, ldv, lde):
-        self.values, self.exponents, self.rows, self.cols = values, exponents, rows, cols
-        self.device = values.device
-        self._held = _Block8(values.data_ptr(), exponents.data_ptr(), rows, cols, ldv, lde)
+        self.rows, self.cols, self.device, self._flat = rows, cols, values.device, None
+        self._values, self._exponents = values, exponents
+        self._held = _Block8(pv, pe, rows, cols, ldv, lde)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Checkpoint":
         """Room for rows x cols values, to be written."""
         width, held = _padded(cols)
         c = cls.__new__(cls)
-        c._set(torch.empty((rows, width), dtype=torch.float8_e4m3fn, device=device),
-               torch.empty((rows, held), dtype=torch.uint8, device=device), rows, cols, width, held)
+        c._flat = flat = torch.empty(rows * (width + held), dtype=torch.uint8, device=device)
+        c._values = c._exponents = None
+        c.rows, c.cols, c.device = rows, cols, flat.device
+        at = flat.data_ptr()
+        c._held = _Block8(at, at + rows * width, rows, cols, width, held)
         return c
+
+    def _part(self, width: int, at: int) -> torch.Tensor:
+        return self._flat[at:at + self.rows * width].view(self.rows, width)
+
+    @property
+    def values(self) -> torch.Tensor:
+        if self._values is None:
+            self._values = self._part(_padded(self.cols)[0], 0).view(torch.float8_e4m3fn)
+        return self._values
+
+    @property
+    def exponents(self) -> torch.Tensor:
+        if self._exponents is None:
+            width, held = _padded(self.cols)
+            self._exponents = self._part(held, self.rows * width)
+        return self._exponents
 
     def restore(self, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """The values, rounded once to dtype (bfloat16 and float32 hold them exactly)."""
@@ -174,11 +189,11 @@ class Checkpoint:
 
 def checkpoint(x: torch.Tensor, transposed: bool = False) -> Checkpoint:
     """x (or its transpose) in 8-bit blocks of 128 values along a row of the result."""
-    x = _matrix(x, "x")
-    rows, cols = x.shape
-    c = Checkpoint.empty(*((cols, rows) if transposed else (rows, cols)), x.device)
-    _run("garfield_checkpoint", x.device, x.data_ptr(), TYPES[x.dtype], rows, cols, _ld(x),
-         int(transposed), c._held)
+    rows, cols, ld, kind = _matrix(x, "x")
+    dev = x.device
+    c = Checkpoint.empty(cols, rows, dev) if transposed else Checkpoint.empty(rows, cols, dev)
+    _run("garfield_checkpoint", dev, x.data_ptr(), kind, rows, cols, ld, 1 if transposed else 0,
+         c._held)
     return c
 
 
@@ -192,12 +207,7 @@ class LayerNorm(NamedTuple):
     x8: Checkpoint | None
 
 
-def _weights(x, weight, bias):
-    kinds = (torch.float32,) if x.dtype == torch.float32 else (torch.float32, x.dtype)
-    weight = _vector(weight, "weight", x.shape[1], kinds, x.device)
-    if bias is not None:
-        bias = _vector(bias, "bias", x.shape[1], (weight.dtype,), x.device)
-    return weight, bias
+_WEIGHTS = {t: (torch.float32,) if t == torch.float32 else (torch.float32, t) for t in TYPES}
 
 
 def layernorm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None,
@@ -205,17 +215,17 @@ def layernorm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
               x8: bool = False) -> LayerNorm:
     """Layer norm of each row of x: (x - mean) * rstd * weight + bias in x's type
     (y) and in 8-bit blocks (y8), and x itself in 8-bit blocks (x8)."""
-    x = _matrix(x, "x")
-    weight, bias = _weights(x, weight, bias)
-    rows, cols = x.shape
-    out = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if y else None
-    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    mean, rstd = stats[0], stats[1]
-    cy = Checkpoint.empty(rows, cols, x.device) if y8 else None
-    cx = Checkpoint.empty(rows, cols, x.device) if x8 else None
-    _run("garfield_layernorm", x.device, x.data_ptr(), TYPES[x.dtype], rows, cols, _ld(x),
-         weight.data_ptr(), _ptr(bias), TYPES[weight.dtype], eps, _ptr(out), max(cols, 1),
-         mean.data_ptr(), rstd.data_ptr(), cy._held if y8 else None, cx._held if x8 else None)
+    rows, cols, ld, kind = _matrix(x, "x")
+    dev, dtype = x.device, x.dtype
+    pw = _vector(weight, "weight", cols, _WEIGHTS[dtype], dev)
+    pb = None if bias is None else _vector(bias, "bias", cols, (weight.dtype,), dev)
+    out = torch.empty((rows, cols), dtype=dtype, device=dev) if y else None
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    cy = Checkpoint.empty(rows, cols, dev) if y8 else None
+    cx = Checkpoint.empty(rows, cols, dev) if x8 else None
+    _run("garfield_layernorm", dev, x.data_ptr(), kind, rows, cols, ld, pw, pb,
+         TYPES[weight.dtype], eps, out.data_ptr() if y else None, cols, mean.data_ptr(),
+         rstd.data_ptr(), cy._held if y8 else None, cx._held if x8 else None)
     return LayerNorm(out, mean, rstd, cy, cx)
 
 
@@ -231,20 +241,25 @@ def _rows_of_workers(out, name: str, shape, device):
     """The caller's rows of the gradients, or new ones; and their distance."""
     if out is None:
         out = torch.empty(shape, dtype=torch.float32, device=device)
-    length = 1
-    for s in shape[1:]:
-        length *= s
-    inner = out[0] if isinstance(out, torch.Tensor) and out.dim() == len(shape) and shape[0] else None
-    if (inner is None or tuple(out.shape) != tuple(shape) or out.dtype != torch.float32
-            or out.device != device or not inner.is_contiguous()
-            or (shape[0] > 1 and out.stride(0) < length)):
+    length = shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    if not isinstance(out, torch.Tensor) or out.shape != shape or out.dtype != torch.float32 \
+            or out.device != device:
+        fine = False
+    else:
+        ld, *inner = out.stride()
+        if shape[0] == 1:
+            ld = length
+        # columns next to each other, and rows of a matrix too, where there is more than one
+        fine = (ld >= length and (inner[-1] == 1 or shape[-1] < 2)
+                and (len(shape) == 2 or inner[0] == shape[2] or shape[1] < 2)) or length == 0
+    if not fine:
         raise ValueError(f"{name} must be a float32 tensor of {tuple(shape)} on {device}, each "
                          "worker's values next to each other")
-    return out, out.stride(0) if shape[0] > 1 else length
+    return out, ld
 
 
 def _workspace(name: str, device, *args):
-    need = (_fn[name] if _fn else _functions()[name])(*args)
+    need = (_fn.get(name) or _functions()[name])(*args)
     return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
 
 
@@ -255,28 +270,26 @@ def layernorm_backward(dy: torch.Tensor, x, mean: torch.Tensor, rstd: torch.Tens
     type or as a Checkpoint; counts the tokens of each of the n workers (None: one
     worker). dweight and dbias (n x cols, float32) may be given, e.g. columns of
     the matrix of gradients."""
-    dy = _matrix(dy, "dy")
-    rows, cols = dy.shape
+    rows, cols, ld, kind = _matrix(dy, "dy")
     dev = dy.device
-    x8 = x if isinstance(x, Checkpoint) else None
-    if x8 is None:
-        x = _matrix(x, "x", dy.dtype)
-    if (tuple((x8.rows, x8.cols) if x8 is not None else x.shape) != (rows, cols)
-            or x.device != dev):
+    if isinstance(x, Checkpoint):
+        px, ldx, x8, shape = None, 0, x._held, (x.rows, x.cols)
+    else:
+        r, c, ldx, _ = _matrix(x, "x", dy.dtype)
+        px, x8, shape = x.data_ptr(), None, (r, c)
+    if shape != (rows, cols) or x.device != dev:
         raise ValueError("x must have dy's shape and device")
-    mean = _vector(mean, "mean", rows, (torch.float32,), dev)
-    rstd = _vector(rstd, "rstd", rows, (torch.float32,), dev)
-    weight, _ = _weights(dy, weight, None)
-    n, c = _counted(counts, rows)
+    pm = _vector(mean, "mean", rows, (torch.float32,), dev)
+    pr = _vector(rstd, "rstd", rows, (torch.float32,), dev)
+    pw = _vector(weight, "weight", cols, _WEIGHTS[dy.dtype], dev)
+    n, counts = _counted(counts, rows)
     dweight, ldw = _rows_of_workers(dweight, "dweight", (n, cols), dev)
     dbias, ldb = _rows_of_workers(dbias, "dbias", (n, cols), dev)
     dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
-    ws, need = _workspace("garfield_layernorm_backward_workspace", dev, rows, cols, n, c)
-    _run("garfield_layernorm_backward", dev, dy.data_ptr(), TYPES[dy.dtype], rows, cols, _ld(dy),
-         None if x8 is not None else x.data_ptr(), 0 if x8 is not None else _ld(x),
-         None if x8 is None else x8._held, mean.data_ptr(), rstd.data_ptr(), weight.data_ptr(),
-         TYPES[weight.dtype], dx.data_ptr(), max(cols, 1), n, c, dweight.data_ptr(), ldw,
-         dbias.data_ptr(), ldb, _ptr(ws), need)
+    ws, need = _workspace("garfield_layernorm_backward_workspace", dev, rows, cols, n, counts)
+    _run("garfield_layernorm_backward", dev, dy.data_ptr(), kind, rows, cols, ld, px, ldx, x8, pm,
+         pr, pw, TYPES[weight.dtype], dx.data_ptr(), cols, n, counts, dweight.data_ptr(), ldw,
+         dbias.data_ptr(), ldb, ws.data_ptr() if need else None, need)
     return dx, dweight, dbias
 
 
@@ -287,16 +300,16 @@ def linear8(x8: Checkpoint, w8: Checkpoint, bias: torch.Tensor | None = None,
     which runs at twice the rate and keeps 14 bits of every eight products."""
     if not isinstance(x8, Checkpoint) or not isinstance(w8, Checkpoint):
         raise ValueError("x8 and w8 must be checkpoints")
-    if x8.cols != w8.cols or x8.device != w8.device:
+    dev, m, n, k = x8.device, x8.rows, w8.rows, x8.cols
+    if k != w8.cols or dev != w8.device:
         raise ValueError("x8 and w8 must have the same columns and device")
     if dtype not in TYPES:
         raise ValueError("dtype must be float32, bfloat16 or float16")
-    if bias is not None:
-        bias = _vector(bias, "bias", w8.rows, (torch.float32,), x8.device)
-    out = torch.empty((x8.rows, w8.rows), dtype=dtype, device=x8.device)
-    ws, need = _workspace("garfield_linear8_workspace", x8.device, x8.rows, w8.rows, x8.cols)
-    _run("garfield_linear8", x8.device, x8._held, w8._held, _ptr(bias), int(fast), out.data_ptr(),
-         TYPES[dtype], max(w8.rows, 1), _ptr(ws), need)
+    pb = None if bias is None else _vector(bias, "bias", n, (torch.float32,), dev)
+    out = torch.empty((m, n), dtype=dtype, device=dev)
+    ws, need = _workspace("garfield_linear8_workspace", dev, m, n, k)
+    _run("garfield_linear8", dev, x8._held, w8._held, pb, 1 if fast else 0, out.data_ptr(),
+         TYPES[dtype], n or 1, ws.data_ptr() if need else None, need)
     return out
 
 
@@ -307,19 +320,19 @@ def weight_gradient(dy: torch.Tensor, x8: Checkpoint, counts=None,
     the gradient of the layer's output; x8: the checkpoint of its input; out and
     dbias may be given, e.g. columns of the matrix of gradients (dbias is None
     where it is not given)."""
-    dy = _matrix(dy, "dy")
-    tokens, outputs = dy.shape
+    tokens, outputs, ld, kind = _matrix(dy, "dy")
     dev = dy.device
     if not isinstance(x8, Checkpoint) or x8.rows != tokens or x8.device != dev:
         raise ValueError("x8 must be a checkpoint with dy's rows and device")
-    n, c = _counted(counts, tokens)
-    out, ld = _rows_of_workers(out, "out", (n, outputs, x8.cols), dev)
-    ldb = outputs
+    n, counts = _counted(counts, tokens)
+    out, ldw = _rows_of_workers(out, "out", (n, outputs, x8.cols), dev)
+    pb, ldb = None, 0
     if dbias is not None:
         dbias, ldb = _rows_of_workers(dbias, "dbias", (n, outputs), dev)
-    kind = TYPES[dy.dtype]
-    ws, need = _workspace("garfield_weight_gradient_workspace", dev, dy.data_ptr(), kind, tokens,
-                          outputs, x8.cols, _ld(dy), n, c)
-    _run("garfield_weight_gradient", dev, dy.data_ptr(), kind, tokens, outputs, _ld(dy), x8._held,
-         n, c, out.data_ptr(), ld, _ptr(dbias), ldb, _ptr(ws), need)
+        pb = dbias.data_ptr()
+    py = dy.data_ptr()
+    ws, need = _workspace("garfield_weight_gradient_workspace", dev, py, kind, tokens, outputs,
+                          x8.cols, ld, n, counts)
+    _run("garfield_weight_gradient", dev, py, kind, tokens, outputs, ld, x8._held, n, counts,
+         out.data_ptr(), ldw, pb, ldb, ws.data_ptr() if need else None, need)
     return out, dbias
