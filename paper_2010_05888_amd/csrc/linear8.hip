@@ -162,8 +162,11 @@ __device__ __forceinline__ Place place_of(uint32_t id, uint32_t total, uint32_t 
 // FA x FB products of 16 x 16, block after block of 128 columns. The next
 // block's codes go from memory straight to LDS while the waves work on this one,
 // the exponents of four blocks with every fourth of them.
-// A row of 128 codes is eight 16-byte chunks, chunk c at c ^ (row % 8), so that the
-// rows that a wave reads together lie in different banks. Lane l takes chunks
+// A row of 128 codes is eight 16-byte chunks, chunk c at c ^ (row / 2 % 8). Lane l
+// takes chunks l / 16 and l / 16 + 4 of its rows. LDS serves 16 lanes of a 16-byte
+// read at a time, from two neighbouring groups of 16 lanes the even quarters of
+// one and the odd ones of the other; two rows are the banks' 256 bytes, and so each
+// lane reads banks of its own. Lane l takes chunks
 // 2 (l / 16) and 2 (l / 16) + 1 of its rows.
 // Offset: of a row from its tile's first one.
 template <typename T, bool FAST, typename Offset, int WJ, int WM, int FA, int FB>
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
     const int last = of_w ? left_j : left_m;
     row = row < last ? row : last;
     from[i] = static_cast<Offset>(row) * static_cast<Offset>(of_w ? w.ld_values : x.ld_values) +
-              ((lane % 8) ^ (lane / 8)) * 16;
+              ((lane % 8) ^ ((i * kWaves + wave) * 4 + lane / 16) % 8) * 16;
   }
   static_assert(kLoads * kTileJ % kRows == 0, "a load is of W's rows or of X's");
   const uint8_t* e0;
@@ -231,13 +234,12 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
     for (int k = 0; k < FB; ++k) sum[i][k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
   const int blocks = static_cast<int>((x.cols + kBlock8 - 1) / kBlock8);
-  const int row0 = lane % 16 * kBlock8, chunk0 = (lane / 16 * 2) ^ (lane % 8);
-  const int near0 = row0 + chunk0 * 16, near1 = row0 + (chunk0 ^ 1) * 16;
+  const int row0 = lane % 16 * kBlock8, chunk0 = (lane / 16) ^ (lane % 16 / 2);
+  const int near0 = row0 + chunk0 * 16, near1 = row0 + (chunk0 ^ 4) * 16;
   uint32_t ew[FA], ex[FB];
   if (blocks > 0) fetch(0);
   for (int b = 0; b < blocks; ++b) {
     __syncthreads();  // block b is there, and block b - 1 has been read
-    if (b + 1 < blocks) fetch(b + 1);
     if (b % 4 == 0) {
       const uint32_t* e = reinterpret_cast<const uint32_t*>(lds + 2 * kCodes +
                                                             (b / 4 & 1) * kExponents) + lane % 16;
@@ -263,6 +265,7 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
 #pragma unroll
       for (int k = 0; k < FB; ++k) xf[k] = read(xt + k * 16 * kBlock8);
       wf[0] = read(wt);
+      if (b + 1 < blocks) fetch(b + 1);
 #pragma unroll
       for (int i = 0; i < FA; ++i) {
         if (i + 1 < FA) wf[(i + 1) & 1] = read(wt + (i + 1) * 16 * kBlock8);
@@ -273,6 +276,7 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
       }
     } else {
       // a quarter of the lane's codes at a time
+      if (b + 1 < blocks) fetch(b + 1);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int near = (q < 2 ? near0 : near1) + q % 2 * 8;

@@ -36,7 +36,7 @@ __device__ __forceinline__ void load_to_lds16(u4 buffer, uint32_t from, uint32_t
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(buffer)
-               : "memory", "m0");
+               : "memory");
 }
 
 // One byte a lane, to the low byte of a word of LDS at to + 4 * lane (the others 0).
@@ -44,7 +44,7 @@ __device__ __forceinline__ void load_to_lds1(u4 buffer, uint32_t from, uint32_t 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, 0 offen lds"
                :
                : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(buffer)
-               : "memory", "m0");
+               : "memory");
 }
 
 template <int N>

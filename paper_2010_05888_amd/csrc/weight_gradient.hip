@@ -10,6 +10,8 @@
 // waves; dY goes straight to LDS. Two workgroups share a CU, so that one's
 // products cover the other's stores: dw is 4 bytes for 2 tokens operations.
 
+#include <cstdlib>
+
 #include "block8.h"
 #include "internal.h"
 #include "timing.h"
@@ -85,42 +87,50 @@ struct Parts {
 
 constexpr int kTokens = 32;  // a step's: the matrix instruction's depth
 
+// (Rows of four chunks: two of them are the banks' 256 bytes.)
+template <int CHUNKS>
+__device__ __forceinline__ int spread(int t) {
+  return CHUNKS == 4 ? (t >> 1 & 1) | (t >> 2 & 2) : (t & 3) | (t >> 1 & 4);
+}
+
 // Four values of a column for each lane's column: 16 lanes read 4 rows of 16
 // neighbouring columns, lane l from row l / 4 and column l % 4 * 4 on, and lane l
 // gets column l's.
-__device__ __forceinline__ bf4 read_column(const uint8_t* p) {
+typedef __attribute__((address_space(3))) uint8_t* LocalBytes;
+__device__ __forceinline__ bf4 read_column(LocalBytes p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-      (__attribute__((address_space(3))) bf4*)(LocalPtr)p);
+      reinterpret_cast<__attribute__((address_space(3))) bf4*>(p));
 }
 
 __device__ __forceinline__ bf8 join(bf4 a, bf4 b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// A workgroup makes 64 * FB outputs x 128 inputs of one worker's gradient, a wave
-// 16 * FB of the outputs, step after step of 32 tokens. While step s is
+// A workgroup makes 64 * FB outputs x 128 * WK inputs of one worker's gradient, a
+// wave 16 * FB x 128 of them, step after step of 32 tokens. While step s is
 // multiplied, step s + 2 is on its way to LDS; then every thread turns its 16 codes
 // of step s + 1 into bf16. So dY has three places, X's codes two, its values two.
-// Rows of 32-byte chunks (16 values), chunk c of token t at c ^ (t % 8) (t % 4 where
-// a row has four): the four rows that 16 lanes read lie in different banks.
+// Rows are 32-byte chunks of 16 values, and 32 lanes read a chunk of tokens t to
+// t + 3 and t + 8 to t + 11 at a time: chunk c of token t lies at c ^ spread(t), which
+// gives each its own eighth of the banks.
 // Tokens past the worker's last read as 0 in both operands.
-template <int FB>
-__global__ __launch_bounds__(256, 2) void k_weight_gradient(Parts a, garfield_block8 x,
-                                                            Tokens tokens, float* __restrict__ dw,
-                                                            int64_t ld_dw,
-                                                            float* __restrict__ dbias,
-                                                            int64_t ld_dbias, int64_t outputs,
-                                                            uint32_t tiles_j, uint32_t tiles_k) {
-  constexpr int kFA = 8, kTileJ = 64 * FB, kTileK = 128;
+template <int WK, int FB>
+__global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
+    Parts a, garfield_block8 x, Tokens tokens, float* __restrict__ dw, int64_t ld_dw,
+    float* __restrict__ dbias, int64_t ld_dbias, int64_t outputs, uint32_t tiles_j,
+    uint32_t tiles_k) {
+  constexpr int kFA = 8, kWaves = 4 * WK, kTileJ = 64 * FB, kTileK = 128 * WK;
   constexpr int kRowJ = kTileJ * 2, kRowK = kTileK * 2;  // bytes
   constexpr int kY = kTokens * kRowJ, kX = kTokens * kRowK, kCodes = kTokens * kTileK;
-  constexpr int kExponents = 4 * 256;  // a word a thread
+  constexpr int kExponents = 256 * kWaves;  // a word a thread
   constexpr int kAtX = 3 * kY, kAtCodes = kAtX + 2 * kX, kAtExponents = kAtCodes + 2 * kCodes;
-  constexpr int kMaskJ = FB == 1 ? 3 : 7;
   constexpr int kFetchRows = 1024 / kRowJ;  // rows that a wave's load brings
-  constexpr int kFetches = FB + 2;          // a step's loads of a wave
+  constexpr int kLoads = FB / WK;           // of dY, a wave and step
+  constexpr int kFetches = kLoads + 2;
+  static_assert(FB % WK == 0, "loads are shared out evenly");
   __shared__ __align__(1024) uint8_t lds[kAtExponents + 2 * kExponents];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wj = wave % 4, wk = wave / 4;
 
   // an XCD's share of the tiles is contiguous (workgroups go to the XCDs in turn)
   const uint32_t total = gridDim.x, share = total / 8, more = total % 8, xcd = blockIdx.x % 8;
@@ -128,69 +138,89 @@ __global__ __launch_bounds__(256, 2) void k_weight_gradient(Parts a, garfield_bl
   const int worker = at / (tiles_j * tiles_k);
   at %= tiles_j * tiles_k;
   const int64_t j0 = static_cast<int64_t>(at % tiles_j) * kTileJ;
-  const int block = at / tiles_j;
+  const int block0 = at / tiles_j * WK;
   const int64_t first = tokens.first[worker], end = tokens.first[worker + 1];
-  const int64_t steps = (end - first + kTokens - 1) / kTokens * a.parts;
+  const int64_t per_part = (end - first + kTokens - 1) / kTokens, steps = per_part * a.parts;
 
   // the lane's places in a step of dY, X and X's exponents
-  uint32_t from[FB];
+  uint32_t from[kLoads];
 #pragma unroll
-  for (int i = 0; i < FB; ++i) {
-    const int t = (i * 4 + wave) * kFetchRows + lane * 16 / kRowJ;
+  for (int i = 0; i < kLoads; ++i) {
+    const int t = (i * kWaves + wave) * kFetchRows + lane * 16 / kRowJ;
     const int piece = lane % (kRowJ / 16);
-    const int column = (((piece / 2) ^ (t & kMaskJ)) * 2 + piece % 2) * 8;
+    const int column = (((piece / 2) ^ spread<4 * FB>(t)) * 2 + piece % 2) * 8;
     from[i] = (static_cast<uint32_t>(t) * static_cast<uint32_t>(a.ld) + column) * 2;
   }
-  const int xt = threadIdx.x / 8, xp = threadIdx.x % 8;  // eight threads to a token
+  const int xt = threadIdx.x / (8 * WK), xp = threadIdx.x % (8 * WK);  // a token's 16 codes
   const uint32_t from_x = static_cast<uint32_t>(xt) * static_cast<uint32_t>(x.ld_values) + xp * 16;
-  const uint32_t from_e = static_cast<uint32_t>(xt) * static_cast<uint32_t>(x.ld_exponents);
+  const uint32_t from_e =
+      static_cast<uint32_t>(xt) * static_cast<uint32_t>(x.ld_exponents) + xp / 8;
   const uint32_t base = lds_offset(lds);
 
-  int64_t fetch_t = first, fetched = 0;  // the step to be fetched
-  const __bf16* part = a.dy;
-  auto fetch = [&](int place) {
-    const int64_t left = end - fetch_t;
-    const uint32_t rows =
-        fetched >= steps ? 0 : static_cast<uint32_t>(left < kTokens ? left : kTokens);
-    const uint32_t beyond = rows ? rows - 1 : 0;  // rows before the last
-    const u4 of_y = buffer_of(part + fetch_t * a.ld + j0,
-                              rows ? (beyond * static_cast<uint32_t>(a.ld) +
-                                      static_cast<uint32_t>(a.columns - j0)) * 2
-                                   : 0);
-    const u4 of_x = buffer_of(x.values + fetch_t * x.ld_values + block * kTileK,
-                              rows ? beyond * static_cast<uint32_t>(x.ld_values) + kTileK : 0);
-    const u4 of_e = buffer_of(x.exponents + fetch_t * x.ld_exponents + block,
-                              rows ? beyond * static_cast<uint32_t>(x.ld_exponents) + 1 : 0);
+  // What the next fetch reads. The bounds of a part's last step end its rows at the
+  // worker's last token; X's end at its last block, for a tile may reach beyond.
+  const int blocks = static_cast<int>((x.cols + kBlock8 - 1) / kBlock8);
+  const int here = blocks - block0 < WK ? blocks - block0 : WK;
+  const uint32_t rows_before =
+      static_cast<uint32_t>(end - first - (per_part - 1) * kTokens) - 1;  // the last one
+  const uint32_t last_y = (rows_before * static_cast<uint32_t>(a.ld) +
+                           static_cast<uint32_t>(a.columns - j0)) * 2;
+  const uint32_t last_x = rows_before * static_cast<uint32_t>(x.ld_values) + here * kBlock8;
+  const uint32_t last_e = rows_before * static_cast<uint32_t>(x.ld_exponents) + here;
+  const uint32_t full_y = ((kTokens - 1) * static_cast<uint32_t>(a.ld) +
+                           static_cast<uint32_t>(a.columns - j0)) * 2;
+  const uint32_t full_x =
+      (kTokens - 1) * static_cast<uint32_t>(x.ld_values) + here * kBlock8;
+  const uint32_t full_e = (kTokens - 1) * static_cast<uint32_t>(x.ld_exponents) + here;
+  const __bf16* at_y = a.dy + first * a.ld + j0;
+  const uint8_t* at_x = x.values + first * x.ld_values + static_cast<int64_t>(block0) * kBlock8;
+  const uint8_t* at_e = x.exponents + first * x.ld_exponents + block0;
+  int64_t left = per_part, parts_left = steps > 0 ? a.parts : 0;
+  auto fetch = [&](int place, int odd) {
+    const bool last = left == 1, none = parts_left <= 0;  // two fetches go past the end
+    const u4 of_y = buffer_of(at_y, none ? 0 : last ? last_y : full_y);
+    const u4 of_x = buffer_of(at_x, none ? 0 : last ? last_x : full_x);
+    const u4 of_e = buffer_of(at_e, none ? 0 : last ? last_e : full_e);
 #pragma unroll
-    for (int i = 0; i < FB; ++i)
-      load_to_lds16(of_y, from[i], base + place * kY + (i * 4 + wave) * 1024);
-    const int odd = fetched & 1;
+    for (int i = 0; i < kLoads; ++i)
+      load_to_lds16(of_y, from[i], base + place * kY + (i * kWaves + wave) * 1024);
     load_to_lds16(of_x, from_x, base + kAtCodes + odd * kCodes + wave * 1024);
     load_to_lds1(of_e, from_e, base + kAtExponents + odd * kExponents + wave * 256);
-    ++fetched;
-    fetch_t += kTokens;
-    if (fetch_t >= end) {
-      fetch_t = first;
-      part += a.next;
+    at_y += kTokens * a.ld;
+    at_x += kTokens * x.ld_values;
+    at_e += kTokens * x.ld_exponents;
+    if (--left == 0) {
+      left = per_part;
+      --parts_left;
+      at_y += a.next - per_part * kTokens * a.ld;
+      at_x -= per_part * kTokens * x.ld_values;
+      at_e -= per_part * kTokens * x.ld_exponents;
     }
   };
   // the thread's own codes, as its wave has fetched them
-  auto decode = [&](int odd) {
+  struct Codes {
+    u4 code;
+    uint32_t exponent;
+  };
+  auto read_codes = [&](int odd) {
+    return Codes{
+        *reinterpret_cast<const u4*>(lds + kAtCodes + odd * kCodes + threadIdx.x * 16),
+        *reinterpret_cast<const uint32_t*>(lds + kAtExponents + odd * kExponents + threadIdx.x * 4)};
+  };
+  const int to_x = xt * kRowK + (xp ^ spread<8>(xt)) * 32;
+  auto decode = [&](Codes c, int odd) {
     typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
     union {
       bf2 h[8];
       u4 v[2];
     } t;
-    const u4 code = *reinterpret_cast<const u4*>(lds + kAtCodes + odd * kCodes + threadIdx.x * 16);
-    const uint32_t e = *reinterpret_cast<const uint32_t*>(lds + kAtExponents + odd * kExponents +
-                                                          threadIdx.x * 4);
-    const float scale = __uint_as_float(e << 23);
+    const float scale = __uint_as_float(c.exponent << 23);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      t.h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[i], scale, false);
-      t.h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[i], scale, true);
+      t.h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.code[i], scale, false);
+      t.h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.code[i], scale, true);
     }
-    u4* to = reinterpret_cast<u4*>(lds + kAtX + odd * kX + xt * kRowK + ((xp ^ (xt & 7)) * 32));
+    u4* to = reinterpret_cast<u4*>(lds + kAtX + odd * kX + to_x);
     to[0] = t.v[0];
     to[1] = t.v[1];
   };
@@ -205,74 +235,105 @@ __global__ __launch_bounds__(256, 2) void k_weight_gradient(Parts a, garfield_bl
   bf8 one;
 #pragma unroll
   for (int e = 0; e < 8; ++e) one[e] = static_cast<__bf16>(1.0f);
-  const bool with_bias = dbias && block == 0;
+  const bool with_bias = dbias && block0 == 0 && wk == 0;
 
   // lane's places in a step: token 8 (l / 16) + l % 16 / 4, and four tokens on
   const int t0 = lane / 16 * 8 + lane % 16 / 4, in_chunk = lane % 4 * 8;
-  const int near_j = t0 * kRowJ + (t0 & kMaskJ) * 32 + in_chunk;
-  const int next_j = (t0 + 4) * kRowJ + ((t0 + 4) & kMaskJ) * 32 + in_chunk;
-  const int near_k = t0 * kRowK + (t0 & 7) * 32 + in_chunk;
-  const int next_k = (t0 + 4) * kRowK + ((t0 + 4) & 7) * 32 + in_chunk;
-
-  if (steps > 0) {
-    fetch(0);
-    fetch(1);
-    wait_for<kFetches>();
-    decode(0);
-    barrier();
+  const LocalBytes local = (LocalBytes)lds;
+  LocalBytes near_y[FB], next_y[FB], near_x[kFA], next_x[kFA];
+#pragma unroll
+  for (int k = 0; k < FB; ++k) {
+    const int c = wj * FB + k;
+    near_y[k] = local + t0 * kRowJ + (c ^ spread<4 * FB>(t0)) * 32 + in_chunk;
+    next_y[k] = local + (t0 + 4) * kRowJ + (c ^ spread<4 * FB>(t0 + 4)) * 32 + in_chunk;
   }
-  int place = 0;
-  for (int64_t s = 0; s < steps; ++s) {
-    const int next = place == 2 ? 0 : place + 1;
-    fetch(next == 2 ? 0 : next + 1);
-    const uint8_t* py = lds + place * kY;
-    const uint8_t* px = lds + kAtX + (s & 1) * kX;
-    bf8 y[FB];
 #pragma unroll
-    for (int k = 0; k < FB; ++k) {
-      const int c = (wave * FB + k) * 32;
-      y[k] = join(read_column(py + (near_j ^ c)), read_column(py + (next_j ^ c)));
-    }
+  for (int i = 0; i < kFA; ++i) {
+    const int c = wk * kFA + i;
+    near_x[i] = local + kAtX + t0 * kRowK + (c ^ spread<8>(t0)) * 32 + in_chunk;
+    next_x[i] = local + kAtX + (t0 + 4) * kRowK + (c ^ spread<8>(t0 + 4)) * 32 + in_chunk;
+  }
+
+  auto step = [&](int place, int odd) {
+    const int py = place * kY, px = odd * kX;
+    bf8 y[FB], xf[kFA];
 #pragma unroll
-    for (int i = 0; i < kFA; ++i) {
-      const bf8 xf =
-          join(read_column(px + (near_k ^ (i * 32))), read_column(px + (next_k ^ (i * 32))));
+    for (int k = 0; k < FB; ++k)
+      y[k] = join(read_column(near_y[k] + py), read_column(next_y[k] + py));
+    auto read_x = [&](int i) {
+      xf[i] = join(read_column(near_x[i] + px), read_column(next_x[i] + px));
+    };
+    auto multiply = [&](int i) {
 #pragma unroll
       for (int k = 0; k < FB; ++k)
-        sum[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, y[k], sum[i][k], 0, 0, 0);
+        sum[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], y[k], sum[i][k], 0, 0, 0);
+    };
+    read_x(0);
+    read_x(1);
+    fetch(place == 0 ? 2 : place - 1, odd);
+#pragma unroll
+    for (int i = 2; i < kFA; ++i) {
+      read_x(i);
+      multiply(i - 2);
     }
+    wait_for<kFetches>();  // the next step is there
+    const Codes codes = read_codes(1 - odd);
+    multiply(kFA - 2);
+    multiply(kFA - 1);
     if (with_bias) {
 #pragma unroll
       for (int k = 0; k < FB; ++k)
         ones[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, y[k], ones[k], 0, 0, 0);
     }
-    wait_for<kFetches>();  // step s + 1 is there
-    decode((s + 1) & 1);
+    decode(codes, 1 - odd);
     barrier();
-    place = next;
+  };
+  if (steps > 0) {
+    fetch(0, 0);
+    fetch(1, 1);
+    wait_for<kFetches>();
+    decode(read_codes(0), 0);
+    barrier();
+    int place = 0, odd = 0;
+    for (int64_t s = 0; s < steps; ++s) {
+      step(place, odd);
+      place = place == 2 ? 0 : place + 1;
+      odd = 1 - odd;
+    }
   }
-  wait_for<0>();  // the last loads bring zeros to LDS that is free again after this
+  wait_for<0>();  // the last loads, which bring zeros
+  barrier();      // LDS is free
 
-  // a lane has four neighbouring inputs of one output
+  // A lane has four neighbouring inputs of one output, 16 outputs a wave; by way of the
+  // wave's part of LDS they become whole rows of 128 inputs, 32 lanes each.
   typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
-  const int64_t k0 = static_cast<int64_t>(block) * kTileK + lane / 16 * 4;
+  constexpr int kRow = 128 * 4 + 16;  // bytes; the rest spreads rows over the banks
+  static_assert(kWaves * 16 * kRow <= sizeof(lds), "the waves' parts fit");
+  uint8_t* const own = lds + wave * 16 * kRow;
+  const int64_t k0 = static_cast<int64_t>(block0 + wk) * kBlock8 + lane % 32 * 4;
+  const int64_t left_k = x.cols - k0;
 #pragma unroll
   for (int k = 0; k < FB; ++k) {
-    const int64_t j = j0 + (wave * FB + k) * 16 + lane % 16;
-    if (j >= outputs) continue;
-    if (with_bias && lane < 16) dbias[worker * ld_dbias + j] = ones[k][0];
-    float* row = dw + worker * ld_dw + j * x.cols + k0;
+    const int64_t j = j0 + (wj * FB + k) * 16;
+    if (with_bias && lane < 16 && j + lane < outputs) dbias[worker * ld_dbias + j + lane] = ones[k][0];
 #pragma unroll
-    for (int i = 0; i < kFA; ++i) {
-      if (k0 + i * 16 + 4 <= x.cols) {
-        Four t;
+    for (int i = 0; i < kFA; ++i)
+      *reinterpret_cast<v4f*>(own + lane % 16 * kRow + i * 64 + lane / 16 * 16) = sum[i][k];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = sum[i][k][e];
-        *reinterpret_cast<Four*>(row + i * 16) = t;
+    for (int r = 0; r < 16; r += 2) {
+      const int row = r + lane / 32;
+      const v4f t = *reinterpret_cast<const v4f*>(own + row * kRow + lane % 32 * 16);
+      if (j + row >= outputs) continue;
+      float* to = dw + worker * ld_dw + (j + row) * x.cols + k0;
+      if (left_k >= 4) {
+        Four v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = t[e];
+        *reinterpret_cast<Four*>(to) = v;
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (k0 + i * 16 + e < x.cols) row[i * 16 + e] = sum[i][k][e];
+          if (e < left_k) to[e] = t[e];
       }
     }
   }
@@ -300,12 +361,13 @@ size_t packed_bytes(int type, int64_t tokens, int64_t outputs) {
   return static_cast<size_t>(parts_of_type(type)) * tokens * ((outputs + 7) / 8 * 8) * 2;
 }
 
-template <int FB>
+template <int WK, int FB>
 void launch_gradient(const Parts& p, const WeightGradient& a, const Tokens& tokens, hipStream_t s) {
   const uint32_t tiles_j = static_cast<uint32_t>((a.outputs + 64 * FB - 1) / (64 * FB));
-  const uint32_t tiles_k = static_cast<uint32_t>((a.x.cols + kBlock8 - 1) / kBlock8);
-  launch("weight_gradient", k_weight_gradient<FB>, dim3(tiles_j * tiles_k * a.n), dim3(256), 0, s,
-         p, a.x, tokens, a.dw, a.ld_dw, a.dbias, a.ld_dbias, a.outputs, tiles_j, tiles_k);
+  const uint32_t tiles_k = static_cast<uint32_t>((a.x.cols + 128 * WK - 1) / (128 * WK));
+  launch("weight_gradient", k_weight_gradient<WK, FB>, dim3(tiles_j * tiles_k * a.n),
+         dim3(256 * WK), 0, s, p, a.x, tokens, a.dw, a.ld_dw, a.dbias, a.ld_dbias, a.outputs,
+         tiles_j, tiles_k);
 }
 
 template <typename T>
@@ -337,9 +399,11 @@ void choose_gradient(const WeightGradient& a, const Tokens& tokens, void* worksp
     p.ld = a.lddy;
   }
   const int64_t tiles_k = (a.x.cols + kBlock8 - 1) / kBlock8 * a.n;
-  if ((a.outputs + 255) / 256 * tiles_k >= 512) launch_gradient<4>(p, a, tokens, s);
-  else if ((a.outputs + 127) / 128 * tiles_k >= 512) launch_gradient<2>(p, a, tokens, s);
-  else launch_gradient<1>(p, a, tokens, s);
+  const int64_t wide = (a.x.cols + 255) / 256 * a.n;
+  if ((a.outputs + 255) / 256 * wide >= 256 && !getenv("NOWK")) launch_gradient<2, 4>(p, a, tokens, s);
+  else if ((a.outputs + 255) / 256 * tiles_k >= 512) launch_gradient<1, 4>(p, a, tokens, s);
+  else if ((a.outputs + 127) / 128 * tiles_k >= 512) launch_gradient<1, 2>(p, a, tokens, s);
+  else launch_gradient<1, 1>(p, a, tokens, s);
 }
 
 }  // namespace
