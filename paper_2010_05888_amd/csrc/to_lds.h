@@ -52,6 +52,13 @@ __device__ __forceinline__ void wait_for() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
+__device__ __forceinline__ void wait_for_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+}
+
+// A barrier that waits for none of the wave's accesses.
+__device__ __forceinline__ void barrier_alone() { asm volatile("s_barrier" : : : "memory"); }
+
 // A barrier that waits for the wave's LDS accesses and for none of its loads.
 __device__ __forceinline__ void barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");

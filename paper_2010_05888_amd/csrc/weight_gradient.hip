@@ -10,8 +10,6 @@
 // waves; dY goes straight to LDS. Two workgroups share a CU, so that one's
 // products cover the other's stores: dw is 4 bytes for 2 tokens operations.
 
-#include <cstdlib>
-
 #include "block8.h"
 #include "internal.h"
 #include "timing.h"
@@ -24,8 +22,10 @@ namespace {
 
 typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
 
+// The workers' tokens, each worker's cut into `splits` shares of whole steps.
 struct Tokens {
   int64_t first[kWorkersMax + 1];
+  int n, splits;
 };
 
 // Part p of v: the leading eight significant bits of what the parts before it
@@ -107,13 +107,17 @@ __device__ __forceinline__ bf8 join(bf4 a, bf4 b) {
 }
 
 // A workgroup makes 64 * FB outputs x 128 * WK inputs of one worker's gradient, a
-// wave 16 * FB x 128 of them, step after step of 32 tokens. While step s is
-// multiplied, step s + 2 is on its way to LDS; then every thread turns its 16 codes
-// of step s + 1 into bf16. So dY has three places, X's codes two, its values two.
+// wave 16 * FB x 128 of them, step after step of 32 tokens. In step s, step s + 3
+// starts on its way to LDS; between the products every thread turns its 16 codes of
+// step s + 2 into bf16; and the first operands of step s + 1, which the last step's
+// barrier has made good, are read before this one's. So dY has four places, X's
+// codes two, its values three.
 // Rows are 32-byte chunks of 16 values, and 32 lanes read a chunk of tokens t to
 // t + 3 and t + 8 to t + 11 at a time: chunk c of token t lies at c ^ spread(t), which
 // gives each its own eighth of the banks.
-// Tokens past the worker's last read as 0 in both operands.
+// Tokens past the share's last read as 0 in both operands.
+// A worker's splits are gradients of their own, ld_dw apart like the workers' (and
+// the workers of a split n * ld_dw): k_sum_splits adds them.
 template <int WK, int FB>
 __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
     Parts a, garfield_block8 x, Tokens tokens, float* __restrict__ dw, int64_t ld_dw,
@@ -123,7 +127,7 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
   constexpr int kRowJ = kTileJ * 2, kRowK = kTileK * 2;  // bytes
   constexpr int kY = kTokens * kRowJ, kX = kTokens * kRowK, kCodes = kTokens * kTileK;
   constexpr int kExponents = 256 * kWaves;  // a word a thread
-  constexpr int kAtX = 3 * kY, kAtCodes = kAtX + 2 * kX, kAtExponents = kAtCodes + 2 * kCodes;
+  constexpr int kAtX = 4 * kY, kAtCodes = kAtX + 3 * kX, kAtExponents = kAtCodes + 2 * kCodes;
   constexpr int kFetchRows = 1024 / kRowJ;  // rows that a wave's load brings
   constexpr int kLoads = FB / WK;           // of dY, a wave and step
   constexpr int kFetches = kLoads + 2;
@@ -135,11 +139,17 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
   // an XCD's share of the tiles is contiguous (workgroups go to the XCDs in turn)
   const uint32_t total = gridDim.x, share = total / 8, more = total % 8, xcd = blockIdx.x % 8;
   uint32_t at = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
-  const int worker = at / (tiles_j * tiles_k);
+  const int share_of = at / (tiles_j * tiles_k);  // worker by worker in every split
+  const int worker = share_of % tokens.n;
   at %= tiles_j * tiles_k;
   const int64_t j0 = static_cast<int64_t>(at % tiles_j) * kTileJ;
   const int block0 = at / tiles_j * WK;
-  const int64_t first = tokens.first[worker], end = tokens.first[worker + 1];
+  int64_t first = tokens.first[worker], end = tokens.first[worker + 1];
+  const int64_t all = (end - first + kTokens - 1) / kTokens;
+  const int64_t most = (all + tokens.splits - 1) / tokens.splits * kTokens;
+  first += share_of / tokens.n * most;
+  end = first + most < end ? first + most : end;
+  first = first < end ? first : end;
   const int64_t per_part = (end - first + kTokens - 1) / kTokens, steps = per_part * a.parts;
 
   // the lane's places in a step of dY, X and X's exponents
@@ -208,7 +218,7 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
         *reinterpret_cast<const uint32_t*>(lds + kAtExponents + odd * kExponents + threadIdx.x * 4)};
   };
   const int to_x = xt * kRowK + (xp ^ spread<8>(xt)) * 32;
-  auto decode = [&](Codes c, int odd) {
+  auto decode = [&](Codes c, int place) {
     typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
     union {
       bf2 h[8];
@@ -220,7 +230,7 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
       t.h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.code[i], scale, false);
       t.h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.code[i], scale, true);
     }
-    u4* to = reinterpret_cast<u4*>(lds + kAtX + odd * kX + to_x);
+    u4* to = reinterpret_cast<u4*>(lds + kAtX + place * kX + to_x);
     to[0] = t.v[0];
     to[1] = t.v[1];
   };
@@ -254,51 +264,62 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
     next_x[i] = local + kAtX + (t0 + 4) * kRowK + (c ^ spread<8>(t0 + 4)) * 32 + in_chunk;
   }
 
-  auto step = [&](int place, int odd) {
-    const int py = place * kY, px = odd * kX;
-    bf8 y[FB], xf[kFA];
+  bf8 y[FB], xf[kFA];
+  auto read_y = [&](int place) {
 #pragma unroll
     for (int k = 0; k < FB; ++k)
-      y[k] = join(read_column(near_y[k] + py), read_column(next_y[k] + py));
-    auto read_x = [&](int i) {
-      xf[i] = join(read_column(near_x[i] + px), read_column(next_x[i] + px));
-    };
-    auto multiply = [&](int i) {
+      y[k] = join(read_column(near_y[k] + place * kY), read_column(next_y[k] + place * kY));
+  };
+  auto read_x = [&](int i, int place) {
+    xf[i] = join(read_column(near_x[i] + place * kX), read_column(next_x[i] + place * kX));
+  };
+  auto multiply = [&](int i) {
 #pragma unroll
-      for (int k = 0; k < FB; ++k)
-        sum[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], y[k], sum[i][k], 0, 0, 0);
-    };
-    read_x(0);
-    read_x(1);
-    fetch(place == 0 ? 2 : place - 1, odd);
-#pragma unroll
-    for (int i = 2; i < kFA; ++i) {
-      read_x(i);
-      multiply(i - 2);
-    }
-    wait_for<kFetches>();  // the next step is there
-    const Codes codes = read_codes(1 - odd);
-    multiply(kFA - 2);
-    multiply(kFA - 1);
-    if (with_bias) {
-#pragma unroll
-      for (int k = 0; k < FB; ++k)
-        ones[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, y[k], ones[k], 0, 0, 0);
-    }
-    decode(codes, 1 - odd);
-    barrier();
+    for (int k = 0; k < FB; ++k)
+      sum[i][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], y[k], sum[i][k], 0, 0, 0);
   };
   if (steps > 0) {
     fetch(0, 0);
     fetch(1, 1);
-    wait_for<kFetches>();
+    wait_for<0>();
     decode(read_codes(0), 0);
+    decode(read_codes(1), 1);
+    wait_for_lds();
+    fetch(2, 0);
     barrier();
-    int place = 0, odd = 0;
+    read_y(0);
+    read_x(0, 0);
+    read_x(1, 0);
+    int of_x = 0;  // X's place of step s
     for (int64_t s = 0; s < steps; ++s) {
-      step(place, odd);
-      place = place == 2 ? 0 : place + 1;
-      odd = 1 - odd;
+      const int of_y = s & 3, odd = s & 1;
+      const int next_x = of_x == 2 ? 0 : of_x + 1, after_x = next_x == 2 ? 0 : next_x + 1;
+      fetch((of_y + 3) & 3, 1 - odd);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        read_x(i + 2, of_x);
+        multiply(i);
+      }
+      wait_for<kFetches>();  // step s + 2 is there
+      const Codes codes = read_codes(odd);
+      read_x(6, of_x);
+      read_x(7, of_x);
+      multiply(4);
+      multiply(5);
+      decode(codes, after_x);
+      multiply(6);
+      multiply(7);
+      if (with_bias) {
+#pragma unroll
+        for (int k = 0; k < FB; ++k)
+          ones[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, y[k], ones[k], 0, 0, 0);
+      }
+      wait_for_lds();
+      read_y((s + 1) & 3);
+      read_x(0, next_x);
+      read_x(1, next_x);
+      barrier_alone();
+      of_x = next_x;
     }
   }
   wait_for<0>();  // the last loads, which bring zeros
@@ -315,7 +336,7 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
 #pragma unroll
   for (int k = 0; k < FB; ++k) {
     const int64_t j = j0 + (wj * FB + k) * 16;
-    if (with_bias && lane < 16 && j + lane < outputs) dbias[worker * ld_dbias + j + lane] = ones[k][0];
+    if (with_bias && lane < 16 && j + lane < outputs) dbias[share_of * ld_dbias + j + lane] = ones[k][0];
 #pragma unroll
     for (int i = 0; i < kFA; ++i)
       *reinterpret_cast<v4f*>(own + lane % 16 * kRow + i * 64 + lane / 16 * 16) = sum[i][k];
@@ -324,17 +345,42 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
       const int row = r + lane / 32;
       const v4f t = *reinterpret_cast<const v4f*>(own + row * kRow + lane % 32 * 16);
       if (j + row >= outputs) continue;
-      float* to = dw + worker * ld_dw + (j + row) * x.cols + k0;
+      float* to = dw + share_of * ld_dw + (j + row) * x.cols + k0;
       if (left_k >= 4) {
         Four v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = t[e];
-        *reinterpret_cast<Four*>(to) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<Four*>(to));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (e < left_k) to[e] = t[e];
       }
+    }
+  }
+}
+
+// The splits' gradients added in ascending order: sums of `length` values for each of
+// n workers, `next` values apart in partial (n * next for each split).
+__global__ __launch_bounds__(kBlock) void k_sum_splits(const float* __restrict__ partial,
+                                                       int64_t length, int64_t next, int n,
+                                                       int splits, float* __restrict__ out,
+                                                       int64_t ld) {
+  typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+  if (i >= length) return;
+  const float* p = partial + blockIdx.y * next + i;
+  float* to = out + blockIdx.y * ld + i;
+  if (i + 4 <= length) {
+    Four sum = *reinterpret_cast<const Four*>(p);
+#pragma unroll 4
+    for (int k = 1; k < splits; ++k) sum += *reinterpret_cast<const Four*>(p + k * n * next);
+    *reinterpret_cast<Four*>(to) = sum;
+  } else {
+    for (int e = 0; i + e < length; ++e) {
+      float sum = p[e];
+      for (int k = 1; k < splits; ++k) sum += p[k * n * next + e];
+      to[e] = sum;
     }
   }
 }
@@ -358,21 +404,70 @@ bool packs(int type, int64_t outputs, int64_t lddy, const void* dy) {
 }
 
 size_t packed_bytes(int type, int64_t tokens, int64_t outputs) {
-  return static_cast<size_t>(parts_of_type(type)) * tokens * ((outputs + 7) / 8 * 8) * 2;
+  const size_t bytes =
+      static_cast<size_t>(parts_of_type(type)) * tokens * ((outputs + 7) / 8 * 8) * 2;
+  return (bytes + 255) / 256 * 256;
+}
+
+// How a call is tiled: 64 * fb outputs x 128 * wk inputs, and into how many shares a
+// worker's tokens are cut.
+struct Plan {
+  int wk, fb, splits;
+};
+
+// A round of workgroups costs about their time alone on a CU, which for a step of 32
+// tokens is, in units of the largest tile's: 256 x 256, one a CU, 1; two of 128 x 128 on
+// a CU 0.73 (measured at 16384 x 4096 x 4096: 491 us one round, 718 us two); three of 64 x 128
+// 0.6. Few tiles of many tokens leave CUs idle: their tokens are cut into up to 16
+// shares of at least eight steps, whose sums cost a pass over splits * 4 bytes for
+// each value of dw (as long as some 8 steps).
+Plan plan_gradient(int parts, int64_t tokens, int64_t outputs, int64_t inputs, int n) {
+  struct Shape {
+    int wk, fb, slots;
+    double time;
+  };
+  static constexpr Shape kShapes[] = {{2, 4, 1, 1.0}, {1, 2, 2, 0.73}, {1, 1, 3, 0.6}};
+  const int cus = device_cus();
+  const double steps = static_cast<double>((tokens / n + kTokens) / kTokens) * parts;
+  Plan best = {1, 1, 1};
+  double least = 1e300;
+  for (const Shape& f : kShapes) {
+    const int64_t tiles = ((outputs + 64 * f.fb - 1) / (64 * f.fb)) *
+                          ((inputs + 128 * f.wk - 1) / (128 * f.wk)) * n;
+    for (int splits = 1; splits <= 16; splits *= 2) {
+      if (splits > 1 && (steps < 8.0 * splits || splits * tiles > 4 * f.slots * cus)) break;
+      const int64_t slots = static_cast<int64_t>(f.slots) * cus;
+      const double rounds = static_cast<double>((tiles * splits + slots - 1) / slots);
+      const double sums = splits > 1 ? 8.0 + splits : 0.0;
+      const double time = rounds * f.time * (steps / splits + 4.0) + sums;
+      if (time < least) {
+        least = time;
+        best = {f.wk, f.fb, splits};
+      }
+    }
+  }
+  return best;
 }
 
 template <int WK, int FB>
-void launch_gradient(const Parts& p, const WeightGradient& a, const Tokens& tokens, hipStream_t s) {
+void launch_gradient(const Parts& p, const WeightGradient& a, const Tokens& tokens, float* dw,
+                     int64_t ld_dw, float* dbias, int64_t ld_dbias, hipStream_t s) {
   const uint32_t tiles_j = static_cast<uint32_t>((a.outputs + 64 * FB - 1) / (64 * FB));
   const uint32_t tiles_k = static_cast<uint32_t>((a.x.cols + 128 * WK - 1) / (128 * WK));
-  launch("weight_gradient", k_weight_gradient<WK, FB>, dim3(tiles_j * tiles_k * a.n),
-         dim3(256 * WK), 0, s, p, a.x, tokens, a.dw, a.ld_dw, a.dbias, a.ld_dbias, a.outputs,
-         tiles_j, tiles_k);
+  launch("weight_gradient", k_weight_gradient<WK, FB>,
+         dim3(tiles_j * tiles_k * tokens.n * tokens.splits), dim3(256 * WK), 0, s, p, a.x, tokens,
+         dw, ld_dw, dbias, ld_dbias, a.outputs, tiles_j, tiles_k);
+}
+
+void launch_sums(const float* partial, int64_t length, int64_t next, const Tokens& tokens,
+                 float* out, int64_t ld, hipStream_t s) {
+  launch("sum_splits", k_sum_splits,
+         dim3(static_cast<uint32_t>((length + 4 * kBlock - 1) / (4 * kBlock)), tokens.n),
+         dim3(kBlock), 0, s, partial, length, next, tokens.n, tokens.splits, out, ld);
 }
 
 template <typename T>
-void choose_gradient(const WeightGradient& a, const Tokens& tokens, void* workspace,
-                     hipStream_t s) {
+void choose_gradient(const WeightGradient& a, Tokens& tokens, void* workspace, hipStream_t s) {
   const T* dy = static_cast<const T*>(a.dy);
   if (a.x.cols == 0) {
     if (a.dbias)
@@ -383,6 +478,7 @@ void choose_gradient(const WeightGradient& a, const Tokens& tokens, void* worksp
   }
   Parts p = {};
   p.parts = parts_of<T>();
+  char* rest = static_cast<char*>(workspace);
   if (packs(a.type, a.outputs, a.lddy, a.dy)) {
     const int64_t vectors = (a.outputs + 7) / 8;
     __bf16* packed = static_cast<__bf16*>(workspace);
@@ -393,28 +489,48 @@ void choose_gradient(const WeightGradient& a, const Tokens& tokens, void* worksp
     p.dy = packed;
     p.columns = p.ld = vectors * 8;
     p.next = a.tokens * p.ld;
+    rest += packed_bytes(a.type, a.tokens, a.outputs);
   } else {
     p.dy = static_cast<const __bf16*>(a.dy);
     p.columns = a.outputs;
     p.ld = a.lddy;
   }
-  const int64_t tiles_k = (a.x.cols + kBlock8 - 1) / kBlock8 * a.n;
-  const int64_t wide = (a.x.cols + 255) / 256 * a.n;
-  if ((a.outputs + 255) / 256 * wide >= 256 && !getenv("NOWK")) launch_gradient<2, 4>(p, a, tokens, s);
-  else if ((a.outputs + 255) / 256 * tiles_k >= 512) launch_gradient<1, 4>(p, a, tokens, s);
-  else if ((a.outputs + 127) / 128 * tiles_k >= 512) launch_gradient<1, 2>(p, a, tokens, s);
-  else launch_gradient<1, 1>(p, a, tokens, s);
+  const Plan plan = plan_gradient(p.parts, a.tokens, a.outputs, a.x.cols, a.n);
+  tokens.splits = plan.splits;
+  const int64_t length = a.outputs * a.x.cols;
+  float *dw = a.dw, *dbias = a.dbias;
+  int64_t ld_dw = a.ld_dw, ld_dbias = a.ld_dbias;
+  if (plan.splits > 1) {
+    dw = reinterpret_cast<float*>(rest);
+    ld_dw = (length + 3) / 4 * 4;
+    if (dbias) dbias = dw + plan.splits * a.n * ld_dw;
+    ld_dbias = a.outputs;
+  }
+  if (plan.wk == 2) launch_gradient<2, 4>(p, a, tokens, dw, ld_dw, dbias, ld_dbias, s);
+  else if (plan.fb == 2) launch_gradient<1, 2>(p, a, tokens, dw, ld_dw, dbias, ld_dbias, s);
+  else launch_gradient<1, 1>(p, a, tokens, dw, ld_dw, dbias, ld_dbias, s);
+  if (plan.splits > 1) {
+    launch_sums(dw, length, ld_dw, tokens, a.dw, a.ld_dw, s);
+    if (a.dbias) launch_sums(dbias, a.outputs, a.outputs, tokens, a.dbias, a.ld_dbias, s);
+  }
 }
 
 }  // namespace
 
 size_t weight_gradient_bytes(int type, int64_t tokens, int64_t outputs, int64_t inputs,
-                             const void* dy, int64_t lddy, int, const int64_t*) {
-  return inputs > 0 && packs(type, outputs, lddy, dy) ? packed_bytes(type, tokens, outputs) : 0;
+                             const void* dy, int64_t lddy, int n, const int64_t*) {
+  if (inputs == 0 || outputs == 0) return 0;
+  const size_t packed =
+      packs(type, outputs, lddy, dy) ? packed_bytes(type, tokens, outputs) : 0;
+  const Plan plan = plan_gradient(parts_of_type(type), tokens, outputs, inputs, n);
+  const size_t gradient = static_cast<size_t>((outputs * inputs + 3) / 4 * 4 + outputs);
+  return packed + (plan.splits > 1 ? plan.splits * n * gradient * sizeof(float) : 0);
 }
 
 hipError_t enqueue_weight_gradient(const WeightGradient& a, void* workspace, hipStream_t s) {
   Tokens tokens = {};
+  tokens.n = a.n;
+  tokens.splits = 1;
   for (int w = 0; w < a.n; ++w) tokens.first[w + 1] = tokens.first[w] + a.counts[w];
   if (a.type == GARFIELD_F32) choose_gradient<float>(a, tokens, workspace, s);
   else if (a.type == GARFIELD_BF16) choose_gradient<__bf16>(a, tokens, workspace, s);
