@@ -29,6 +29,22 @@ struct Pack8 {
 };
 
 template <typename T>
+__device__ __forceinline__ void unpack8(const typename Pack8<T>::type& t, float* v) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(t[e]);
+}
+
+// The first `left` of eight elements as they are; the others 0.
+template <typename T>
+__device__ __forceinline__ typename Pack8<T>::type raw8_upto(const T* p, int64_t left) {
+  if (left >= 8) return *reinterpret_cast<const typename Pack8<T>::type*>(p);
+  typename Pack8<T>::type t;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] = e < left ? p[e] : static_cast<T>(0.0f);
+  return t;
+}
+
+template <typename T>
 __device__ __forceinline__ void load8(const T* p, float* v) {
   const auto t = *reinterpret_cast<const typename Pack8<T>::type*>(p);
 #pragma unroll
@@ -98,8 +114,20 @@ __device__ __forceinline__ bool finite(float v) {
   return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
 }
 
-// |v| where it is finite, else 0.
-__device__ __forceinline__ float magnitude(float v) { return finite(v) ? __builtin_fabsf(v) : 0.0f; }
+// The largest finite magnitude of N values. A maximum passes NaN over by itself, so
+// only an infinite one is looked for again.
+template <int N>
+__device__ __forceinline__ float largest(const float* v) {
+  float a = 0.0f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) a = __builtin_fmaxf(a, __builtin_fabsf(v[e]));
+  if (!finite(a)) {
+    a = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) a = __builtin_fmaxf(a, finite(v[e]) ? __builtin_fabsf(v[e]) : 0.0f);
+  }
+  return a;
+}
 
 // s of a block whose largest finite magnitude is a. 448 = 1.75 * 2^8: with
 // a = m * 2^k, s = k - 8 if m <= 1.75, else k - 7.
@@ -118,12 +146,11 @@ __device__ __forceinline__ u2 encode8(const float* v, int s) {
   const float scale = power2(-s);
   float t[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    t[e] = finite(v[e]) ? v[e] * scale : __uint_as_float(0x7fc00000u);
+  for (int e = 0; e < 8; ++e) t[e] = v[e] * scale;  // the cast makes NaN of infinities
   if (s == 120) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (__builtin_fabsf(t[e]) > 240.0f) t[e] = __builtin_copysignf(240.0f, t[e]);
+      if (__builtin_fabsf(t[e]) > 240.0f && finite(t[e])) t[e] = __builtin_copysignf(240.0f, t[e]);
   }
   u2 q;
   int a = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);

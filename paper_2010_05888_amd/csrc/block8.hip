@@ -28,61 +28,84 @@ __global__ __launch_bounds__(kBlock) void k_checkpoint(const T* __restrict__ x, 
   const int64_t c = b * kBlock8 + threadIdx.x % 16 * 8;
   float v[8];
   load8_upto(x + row * ld + c, out.cols - c, v);
-  float a = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) a = __builtin_fmaxf(a, magnitude(v[e]));
-  const int s = block_shift(max16(a));
+  const int s = block_shift(max16(largest<8>(v)));
   *reinterpret_cast<u2*>(out.values + row * out.ld_values + c) = encode8(v, s);
   if (threadIdx.x % 16 == 0)
     out.exponents[row * out.ld_exponents + b] = static_cast<uint8_t>(s + 127);
 }
 
-// The transpose: a workgroup takes 128 rows x 64 columns of x, which are one
-// block of each of 64 rows of the result. Four lanes to a block, 32 values each.
+// The transpose: a workgroup takes 128 rows x 256 bytes of x, the columns of which are
+// one block each of the result's rows; neighbouring workgroups read on in the same
+// rows. Four lanes to a block, 32 values each, and a lane has as many columns as fit
+// a word, which is what it reads from LDS at a time.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_checkpoint_transposed(const T* __restrict__ x,
                                                                   int64_t ld, garfield_block8 out,
-                                                                  int64_t blocks, int64_t padded) {
-  __shared__ float tile[kBlock8][65];
-  const int64_t b = blockIdx.x % padded, r0 = b * kBlock8, c0 = blockIdx.x / padded * 64;
+                                                                  int64_t blocks, int64_t strips) {
+  constexpr int kPer = 4 / sizeof(T), kWords = 64, kCols = kWords * kPer, kVec = 16 / sizeof(T);
+  typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+  union Piece {
+    T t[kVec];
+    uint32_t w[4];
+  };
+  __shared__ uint32_t tile[kBlock8][kWords + 1];
+  const int64_t b = blockIdx.x / strips, r0 = b * kBlock8, c0 = blockIdx.x % strips * kCols;
   if (b >= blocks) {
     const int64_t c = c0 + threadIdx.x;
-    if (threadIdx.x < 64 && c < out.rows) out.exponents[c * out.ld_exponents + b] = 127;
+    if (threadIdx.x < kCols && c < out.rows) out.exponents[c * out.ld_exponents + b] = 127;
     return;
   }
-  for (int r = threadIdx.x / 8; r < kBlock8; r += kBlock / 8) {
-    const int c = threadIdx.x % 8 * 8;
-    float v[8] = {};
-    if (r0 + r < out.cols && c0 + c < out.rows)
-      load8_upto(x + (r0 + r) * ld + c0 + c, out.rows - c0 - c, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) tile[r][c + e] = v[e];
+  for (int i = 0; i < kBlock8 / 16; ++i) {
+    const int r = i * 16 + threadIdx.x / 16, c = threadIdx.x % 16 * kVec;
+    const int64_t left = r0 + r < out.cols ? out.rows - c0 - c : 0;
+    const T* from = x + (r0 + r) * ld + c0 + c;
+    Piece p;
+    if (left >= kVec) {
+      const Vec v = *reinterpret_cast<const Vec*>(from);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) p.t[e] = v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) p.t[e] = e < left ? from[e] : static_cast<T>(0.0f);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[r][threadIdx.x % 16 * 4 + e] = p.w[e];
   }
   __syncthreads();
-  const int col = threadIdx.x / 4, part = threadIdx.x % 4;
-  float v[32];
-  float a = 0.0f;
+  const int word = threadIdx.x / 4, part = threadIdx.x % 4;
+  float v[kPer][32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    v[i] = tile[part * 32 + i][col];
-    a = __builtin_fmaxf(a, magnitude(v[i]));
-  }
-  a = __builtin_fmaxf(a, __shfl_xor(a, 1));
-  a = __builtin_fmaxf(a, __shfl_xor(a, 2));
-  if (c0 + col >= out.rows) return;
-  const int s = block_shift(a);
-  u4* to = reinterpret_cast<u4*>(out.values + (c0 + col) * out.ld_values + r0 + part * 32);
+    union {
+      uint32_t w;
+      T t[kPer];
+    } u;
+    u.w = tile[part * 32 + i][word];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const u2 lo = encode8(v + 16 * i, s), hi = encode8(v + 16 * i + 8, s);
-    u4 q;
-    q.x = lo.x;
-    q.y = lo.y;
-    q.z = hi.x;
-    q.w = hi.y;
-    to[i] = q;
+    for (int e = 0; e < kPer; ++e) v[e][i] = static_cast<float>(u.t[e]);
   }
-  if (part == 0) out.exponents[(c0 + col) * out.ld_exponents + b] = static_cast<uint8_t>(s + 127);
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    float a = largest<32>(v[e]);
+    a = __builtin_fmaxf(a, __shfl_xor(a, 1));
+    a = __builtin_fmaxf(a, __shfl_xor(a, 2));
+    const int64_t row = c0 + word * kPer + e;
+    if (row >= out.rows) continue;
+    const int s = block_shift(a);
+    u4* to = reinterpret_cast<u4*>(out.values + row * out.ld_values + r0 + part * 32);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u2 lo = encode8(v[e] + 16 * i, s), hi = encode8(v[e] + 16 * i + 8, s);
+      u4 q;
+      q.x = lo.x;
+      q.y = lo.y;
+      q.z = hi.x;
+      q.w = hi.y;
+      to[i] = q;
+    }
+    if (part == 0) out.exponents[row * out.ld_exponents + b] = static_cast<uint8_t>(s + 127);
+  }
 }
 
 template <typename T>
@@ -102,10 +125,11 @@ void launch_checkpoint(const void* x, int64_t ld, bool transposed, const garfiel
                        hipStream_t s) {
   const T* p = static_cast<const T*>(x);
   const int64_t blocks = blocks_of(out.cols), padded = padded_blocks(out.cols);
+  const int64_t strips = (out.rows * static_cast<int64_t>(sizeof(T)) + 255) / 256;
   if (transposed)
     launch("checkpoint_transposed", k_checkpoint_transposed<T>,
-           dim3(static_cast<uint32_t>(padded * ((out.rows + 63) / 64))), dim3(kBlock), 0, s, p, ld,
-           out, blocks, padded);
+           dim3(static_cast<uint32_t>(padded * strips)), dim3(kBlock), 0, s, p, ld, out, blocks,
+           strips);
   else
     launch("checkpoint", k_checkpoint<T>,
            dim3(static_cast<uint32_t>((out.rows * padded + kBlock / 16 - 1) / (kBlock / 16))),

@@ -41,6 +41,26 @@ __device__ __forceinline__ float sum_group(float v, float* at) {
   return v;
 }
 
+// The same of R values, with one barrier for all. `at` holds R floats a wave.
+template <int WAVES, int R>
+__device__ __forceinline__ void sums_group(float* v, float (*at)[R]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r) v[r] = sum_wave(v[r]);
+  if constexpr (WAVES > 1) {
+    if (threadIdx.x % 64 == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) at[threadIdx.x / 64][r] = v[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      v[r] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v[r] += at[w][r];
+    }
+  }
+}
+
 // Weights of wtype at p[c..c+7] (cols beyond `left` read as 0).
 template <typename T>
 __device__ __forceinline__ void load_weight(const void* p, bool f32, int64_t c, int64_t left,
@@ -53,10 +73,7 @@ __device__ __forceinline__ void load_weight(const void* p, bool f32, int64_t c, 
 // Called by all 16 lanes of a block.
 __device__ __forceinline__ void store_blocks(const garfield_block8& out, int64_t row, int64_t c,
                                              const float* v) {
-  float a = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) a = __builtin_fmaxf(a, magnitude(v[e]));
-  const int s = block_shift(max16(a));
+  const int s = block_shift(max16(largest<8>(v)));
   const int64_t blocks = (out.cols + kBlock8 - 1) / kBlock8;
   const int64_t b = c / kBlock8;
   if (b < blocks)
@@ -65,57 +82,96 @@ __device__ __forceinline__ void store_blocks(const garfield_block8& out, int64_t
     out.exponents[row * out.ld_exponents + b] = static_cast<uint8_t>(b < blocks ? s + 127 : 127);
 }
 
-// Rows of up to 512 * WAVES * NV columns: a row to WAVES waves, NV vectors of
-// eight to a lane. Workgroups of four waves hold 4 / WAVES rows.
-template <typename T, int WAVES, int NV>
+// Rows of up to 512 * WAVES * NV columns, R rows at a time to a team of WAVES waves,
+// NV vectors of eight of each to a lane. Workgroups of four waves hold 4 / WAVES
+// teams. Several rows at a time share what is read of weight and bias, which is
+// more bytes (from the caches) than the row itself.
+template <typename T, int WAVES, int NV, int R>
 __global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void k_layernorm(LayerNorm a) {
   constexpr int kThreads = 64 * WAVES;
-  constexpr int kRows = WAVES > 4 ? 1 : 4 / WAVES;
-  static_assert(WAVES == 1 || kRows == 1, "barriers are the whole workgroup's");
-  __shared__ float sums[2][WAVES];
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kThreads;
-  if (row >= a.rows) return;  // whole waves, and no barrier where kRows > 1
+  constexpr int kTeams = WAVES > 4 ? 1 : 4 / WAVES;
+  static_assert(WAVES == 1 || kTeams == 1, "barriers are the whole workgroup's");
+  __shared__ float sums[2][WAVES][R];
+  const int64_t row0 = (static_cast<int64_t>(blockIdx.x) * kTeams + threadIdx.x / kThreads) * R;
+  if (row0 >= a.rows) return;  // whole waves, and no barrier where there are several teams
   const int lane = threadIdx.x % kThreads;
-  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  float v[NV][8];
-  float sum = 0.0f;
+  typename Pack8<T>::type x[R][NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int64_t c = (j * kThreads + lane) * 8;
-    load8_upto(x + c, a.cols - c, v[j]);
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = row0 + r < a.rows ? row0 + r : a.rows - 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += v[j][e];
-  }
-  const float mean = sum_group<WAVES>(sum, sums[0]) / static_cast<float>(a.cols);
-  float square = 0.0f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int64_t c = (j * kThreads + lane) * 8;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float t = c + e < a.cols ? v[j][e] - mean : 0.0f;
-      square = __builtin_fmaf(t, t, square);
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * kThreads + lane) * 8;
+      x[r][j] = raw8_upto(static_cast<const T*>(a.x) + row * a.ldx + c, a.cols - c);
     }
   }
-  const float var = sum_group<WAVES>(square, sums[1]) / static_cast<float>(a.cols);
-  const float rstd = 1.0f / __builtin_sqrtf(var + a.eps);
-  if (lane == 0) {
-    a.mean[row] = mean;
-    a.rstd[row] = rstd;
+  float mean[R], rstd[R], v[8];
+  const float scale = 1.0f / static_cast<float>(a.cols);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      unpack8<T>(x[r][j], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += v[e];
+    }
+    mean[r] = sum;
+  }
+  sums_group<WAVES, R>(mean, sums[0]);
+#pragma unroll
+  for (int r = 0; r < R; ++r) mean[r] *= scale;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float square = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t left = a.cols - (j * kThreads + lane) * 8;
+      unpack8<T>(x[r][j], v);
+      if (left >= 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) square = __builtin_fmaf(v[e] - mean[r], v[e] - mean[r], square);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < left) square = __builtin_fmaf(v[e] - mean[r], v[e] - mean[r], square);
+      }
+    }
+    rstd[r] = square;
+  }
+  sums_group<WAVES, R>(rstd, sums[1]);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    rstd[r] = 1.0f / __builtin_sqrtf(rstd[r] * scale + a.eps);
+    if (lane == 0 && row0 + r < a.rows) {
+      a.mean[row0 + r] = mean[r];
+      a.rstd[row0 + r] = rstd[r];
+    }
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int64_t c = (j * kThreads + lane) * 8;
-    if (a.x8.values) store_blocks(a.x8, row, c, v[j]);
-    if (!a.y && !a.y8.values) continue;
+    const int64_t c = (j * kThreads + lane) * 8, left = a.cols - c;
     float w[8], b[8] = {};
-    load_weight<T>(a.weight, a.weight_f32, c, a.cols - c, w);
-    if (a.bias) load_weight<T>(a.bias, a.weight_f32, c, a.cols - c, b);
+    if (a.y || a.y8.values) {
+      load_weight<T>(a.weight, a.weight_f32, c, left, w);
+      if (a.bias) load_weight<T>(a.bias, a.weight_f32, c, left, b);
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      v[j][e] = c + e < a.cols ? __builtin_fmaf((v[j][e] - mean) * rstd, w[e], b[e]) : 0.0f;
-    if (a.y) store8_upto(static_cast<T*>(a.y) + row * a.ldy + c, a.cols - c, v[j]);
-    if (a.y8.values) store_blocks(a.y8, row, c, v[j]);
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = row0 + r;
+      if (row >= a.rows) break;
+      unpack8<T>(x[r][j], v);
+      if (a.x8.values) store_blocks(a.x8, row, c, v);
+      if (!a.y && !a.y8.values) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf((v[e] - mean[r]) * rstd[r], w[e], b[e]);
+      if (left < 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : 0.0f;
+      }
+      if (a.y) store8_upto(static_cast<T*>(a.y) + row * a.ldy + c, left, v);
+      if (a.y8.values) store_blocks(a.y8, row, c, v);
+    }
   }
 }
 
@@ -165,27 +221,32 @@ __global__ __launch_bounds__(1024) void k_layernorm_long(LayerNorm a) {
   }
 }
 
-template <typename T, int WAVES, int NV>
+template <typename T, int WAVES, int NV, int R>
 void launch_layernorm(const LayerNorm& a, hipStream_t s) {
-  constexpr int kRows = WAVES > 4 ? 1 : 4 / WAVES;
-  launch("layernorm", k_layernorm<T, WAVES, NV>,
+  constexpr int kRows = WAVES > 4 ? R : 4 / WAVES * R;
+  launch("layernorm", k_layernorm<T, WAVES, NV, R>,
          dim3(static_cast<uint32_t>((a.rows + kRows - 1) / kRows)),
          dim3(64 * (WAVES > 4 ? WAVES : 4)), 0, s, a);
 }
 
+// With many rows two at a time share the reads of weight and bias and the barriers:
+// 65536 x 4096 in bf16 takes 212 us (5.1 TB/s, a copy's rate), one at a time 242, four
+// 218, and a wave to a row of its own 211, but 74 against 67 at 32768 x 2048 with y8.
 template <typename T>
 void choose_layernorm(const LayerNorm& a, hipStream_t s) {
-  if (a.cols > 65536)
+  const bool many = a.rows >= 8 * device_cus();
+  if (a.cols > 32768)
     launch("layernorm_long", k_layernorm_long<T>, dim3(static_cast<uint32_t>(a.rows)), dim3(1024),
            0, s, a);
-  else if (a.cols > 32768) launch_layernorm<T, 16, 8>(a, s);
-  else if (a.cols > 16384) launch_layernorm<T, 16, 4>(a, s);
-  else if (a.cols > 8192) launch_layernorm<T, 16, 2>(a, s);
-  else if (a.cols > 4096) launch_layernorm<T, 4, 4>(a, s);
-  else if (a.cols > 2048) launch_layernorm<T, 4, 2>(a, s);
-  else if (a.cols > 1024) launch_layernorm<T, 1, 4>(a, s);
-  else if (a.cols > 512) launch_layernorm<T, 1, 2>(a, s);
-  else launch_layernorm<T, 1, 1>(a, s);
+  else if (a.cols > 16384) launch_layernorm<T, 16, 4, 1>(a, s);
+  else if (a.cols > 8192) launch_layernorm<T, 16, 2, 1>(a, s);
+  else if (a.cols > 4096) launch_layernorm<T, 4, 4, 1>(a, s);
+  else if (many && a.cols > 2048) launch_layernorm<T, 4, 2, 2>(a, s);
+  else if (many && a.cols > 1024) launch_layernorm<T, 4, 1, 2>(a, s);
+  else if (a.cols > 2048) launch_layernorm<T, 4, 2, 1>(a, s);
+  else if (a.cols > 1024) launch_layernorm<T, 4, 1, 1>(a, s);
+  else if (a.cols > 512) launch_layernorm<T, 1, 2, 1>(a, s);
+  else launch_layernorm<T, 1, 1, 1>(a, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -215,12 +276,14 @@ __device__ __forceinline__ int worker_of(const Chunks& c, int chunk) {
 
 // A workgroup goes through one chunk of a worker's rows (up to 8 * THREADS * NV
 // columns), its share of the weight's gradient in registers, and writes that to
-// partial[chunk][2][cols]; k_sum_chunks adds the chunks of a worker.
-template <typename T, bool X8, int THREADS, int NV>
+// partial[chunk][2][cols]; k_sum_chunks adds the chunks of a worker. R rows are worked
+// on at a time, with one barrier for their sums, while the next R are on their way.
+template <typename T, bool X8, int THREADS, int NV, int R>
 __global__ __launch_bounds__(THREADS) void k_layernorm_backward(LayerNormBackward a, Chunks chunks,
                                                                 float* partial) {
   constexpr int kWaves = THREADS / 64;
-  __shared__ float sums[2][2][kWaves];
+  typedef typename Pack8<T>::type Raw;
+  __shared__ float sums[2][kWaves][2 * R];
   const int chunk = blockIdx.x;
   const int worker = worker_of(chunks, chunk);
   const int64_t begin = chunks.token0[worker] + (chunk - chunks.chunk0[worker]) * chunks.rows;
@@ -235,52 +298,88 @@ __global__ __launch_bounds__(THREADS) void k_layernorm_backward(LayerNormBackwar
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[j][e] = db[j][e] = 0.0f;
   }
-  for (int64_t row = begin; row < end; ++row) {
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    float g[NV][8], h[NV][8];
-    float along = 0.0f, across = 0.0f;
+  // a row as it lies in memory: dy, and x or its codes and exponents
+  Raw dy[R][NV], x[X8 ? 1 : R][NV];
+  u2 code[X8 ? R : 1][NV];
+  int shift[X8 ? R : 1][NV];
+  float mean[R], rstd[R];
+  auto fetch = [&](int64_t row0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int64_t c = (j * THREADS + threadIdx.x) * 8;
-      load8_upto(static_cast<const T*>(a.dy) + row * a.lddy + c, a.cols - c, g[j]);
-      load_x<T, X8>(a, row, c, h[j]);
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = row0 + r < end ? row0 + r : end - 1;
+      mean[r] = a.mean[row];
+      rstd[r] = a.rstd[row];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        h[j][e] = (h[j][e] - mean) * rstd;
-        dw[j][e] = __builtin_fmaf(g[j][e], h[j][e], dw[j][e]);
-        db[j][e] += g[j][e];
-        g[j][e] *= w[j][e];
-        along += c + e < a.cols ? g[j][e] : 0.0f;
-        across = c + e < a.cols ? __builtin_fmaf(g[j][e], h[j][e], across) : across;
+      for (int j = 0; j < NV; ++j) {
+        const int64_t c = (j * THREADS + threadIdx.x) * 8;
+        dy[r][j] = raw8_upto(static_cast<const T*>(a.dy) + row * a.lddy + c, a.cols - c);
+        if constexpr (X8) {
+          const int64_t at = c < a.cols ? c : 0;
+          code[r][j] = *reinterpret_cast<const u2*>(a.x8.values + row * a.x8.ld_values + at);
+          shift[r][j] = a.x8.exponents[row * a.x8.ld_exponents + at / kBlock8];
+        } else {
+          x[r][j] = raw8_upto(static_cast<const T*>(a.x) + row * a.ldx + c, a.cols - c);
+        }
       }
+    }
+  };
+  fetch(begin);
+  for (int64_t row0 = begin; row0 < end; row0 += R) {
+    float g[R][NV][8], h[R][NV][8], m[R], d[R], both[2 * R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      m[r] = mean[r];
+      d[r] = rstd[r];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        unpack8<T>(dy[r][j], g[r][j]);
+        if constexpr (X8) decode8(code[r][j], power2(shift[r][j] - 127), h[r][j]);
+        else unpack8<T>(x[r][j], h[r][j]);
+      }
+    }
+    if (row0 + R < end) fetch(row0 + R);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float along = 0.0f, across = 0.0f;
+      if (r == 0 || row0 + r < end) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) h[r][j][e] = (h[r][j][e] - m[r]) * d[r];
+          const int64_t left = a.cols - (j * THREADS + threadIdx.x) * 8;
+          if (left < 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[r][j][e] = e < left ? h[r][j][e] : 0.0f;
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            dw[j][e] = __builtin_fmaf(g[r][j][e], h[r][j][e], dw[j][e]);
+            db[j][e] += g[r][j][e];
+            g[r][j][e] *= w[j][e];
+            along += g[r][j][e];
+            across = __builtin_fmaf(g[r][j][e], h[r][j][e], across);
+          }
+        }
+      }
+      both[2 * r] = along;
+      both[2 * r + 1] = across;
     }
     if (!a.dx) continue;
-    // the rows' sums alternate between two places: one barrier a row
-    float* at = sums[(row - begin) & 1][0];
-    along = sum_wave(along);
-    across = sum_wave(across);
-    if constexpr (kWaves > 1) {
-      if (threadIdx.x % 64 == 0) {
-        at[threadIdx.x / 64] = along;
-        at[kWaves + threadIdx.x / 64] = across;
+    // the sums alternate between two places: one barrier for R rows
+    sums_group<kWaves, 2 * R>(both, sums[(row0 - begin) / R & 1]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r > 0 && row0 + r >= end) break;
+      const float along = both[2 * r] * scale, across = both[2 * r + 1] * scale;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int64_t c = (j * THREADS + threadIdx.x) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          g[r][j][e] = d[r] * (g[r][j][e] - along - h[r][j][e] * across);
+        if (c < a.cols)
+          store8_upto(static_cast<T*>(a.dx) + (row0 + r) * a.lddx + c, a.cols - c, g[r][j]);
       }
-      __syncthreads();
-      along = across = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        along += at[i];
-        across += at[kWaves + i];
-      }
-    }
-    along *= scale;
-    across *= scale;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int64_t c = (j * THREADS + threadIdx.x) * 8;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g[j][e] = rstd * (g[j][e] - along - h[j][e] * across);
-      if (c < a.cols)
-        store8_upto(static_cast<T*>(a.dx) + row * a.lddx + c, a.cols - c, g[j]);
     }
   }
   float* out = partial + static_cast<int64_t>(chunk) * 2 * a.cols;
@@ -353,21 +452,28 @@ __global__ __launch_bounds__(64) void k_layernorm_dw_long(LayerNormBackward a, C
   store8_upto(out + a.cols + c, a.cols - c, db);
 }
 
-// The chunks of a worker added in ascending order: column blockIdx.x * 256 +
-// threadIdx.x of partial[chunk][2][cols] for worker blockIdx.y.
+// The chunks of a worker added in one order: column blockIdx.x * 64 + threadIdx.x % 64 of
+// partial[chunk][2][cols] for worker blockIdx.y, every fourth chunk to a wave.
 __global__ __launch_bounds__(kBlock) void k_sum_chunks(const float* __restrict__ partial,
                                                        int64_t cols, Chunks chunks,
                                                        float* __restrict__ dweight,
                                                        int64_t ld_dweight,
                                                        float* __restrict__ dbias,
                                                        int64_t ld_dbias) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
-  if (i >= 2 * cols) return;
-  const int worker = blockIdx.y;
+  __shared__ float sums[4][64];
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x % 64;
+  const int worker = blockIdx.y, part = threadIdx.x / 64;
   float sum = 0.0f;
+  if (i < 2 * cols) {
 #pragma unroll 8
-  for (int c = chunks.chunk0[worker]; c < chunks.chunk0[worker + 1]; ++c)
-    sum += partial[static_cast<int64_t>(c) * 2 * cols + i];
+    for (int c = chunks.chunk0[worker] + part; c < chunks.chunk0[worker + 1]; c += 4)
+      sum += partial[static_cast<int64_t>(c) * 2 * cols + i];
+  }
+  sums[part][threadIdx.x % 64] = sum;
+  __syncthreads();
+  if (part > 0 || i >= 2 * cols) return;
+  sum = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) +
+        (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
   if (i < cols) {
     if (dweight) dweight[worker * ld_dweight + i] = sum;
   } else if (dbias) {
@@ -375,13 +481,13 @@ __global__ __launch_bounds__(kBlock) void k_sum_chunks(const float* __restrict__
   }
 }
 
-template <typename T, bool X8, int THREADS, int NV>
+template <typename T, bool X8, int THREADS, int NV, int R>
 void launch_backward(const LayerNormBackward& a, const Chunks& c, float* partial, hipStream_t s) {
-  launch("layernorm_backward", k_layernorm_backward<T, X8, THREADS, NV>, dim3(c.chunk0[c.n]),
+  launch("layernorm_backward", k_layernorm_backward<T, X8, THREADS, NV, R>, dim3(c.chunk0[c.n]),
          dim3(THREADS), 0, s, a, c, partial);
 }
 
-constexpr int64_t kBackwardMaxCols = 16384;
+constexpr int64_t kBackwardMaxCols = 8192;
 
 template <typename T, bool X8>
 void choose_backward(const LayerNormBackward& a, const Chunks& c, float* partial, hipStream_t s) {
@@ -393,18 +499,16 @@ void choose_backward(const LayerNormBackward& a, const Chunks& c, float* partial
       launch("layernorm_dw_long", k_layernorm_dw_long<T, X8>,
              dim3(static_cast<uint32_t>((a.cols + 511) / 512), c.chunk0[c.n]), dim3(64), 0, s, a,
              c, partial);
-  } else if (a.cols > 8192) {
-    launch_backward<T, X8, 1024, 2>(a, c, partial, s);
   } else if (a.cols > 4096) {
-    launch_backward<T, X8, 512, 2>(a, c, partial, s);
+    launch_backward<T, X8, 512, 2, 1>(a, c, partial, s);
   } else if (a.cols > 2048) {
-    launch_backward<T, X8, 256, 2>(a, c, partial, s);
+    launch_backward<T, X8, 512, 1, 2>(a, c, partial, s);
   } else if (a.cols > 1024) {
-    launch_backward<T, X8, 256, 1>(a, c, partial, s);
+    launch_backward<T, X8, 256, 1, 2>(a, c, partial, s);
   } else if (a.cols > 512) {
-    launch_backward<T, X8, 128, 1>(a, c, partial, s);
+    launch_backward<T, X8, 128, 1, 2>(a, c, partial, s);
   } else {
-    launch_backward<T, X8, 64, 1>(a, c, partial, s);
+    launch_backward<T, X8, 64, 1, 2>(a, c, partial, s);
   }
 }
 
@@ -423,12 +527,20 @@ hipError_t enqueue_layernorm(const LayerNorm& a, int type, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Chunks of equal length, so many that they fill the card: about two
-// workgroups of four waves a CU.
+// Chunks of equal length, as many as the workgroups that the card holds at once (by
+// their registers: 256, 512, 1024, 2048 or 4096 on 256 CUs) and no more: twelve more
+// than 512 cost as much as 512.
 Chunks layernorm_backward_chunks(int64_t rows, int64_t cols, int n, const int64_t* counts) {
-  const int64_t want = cols > 2048 ? 512 : cols > 512 ? 1024 : 2048;
-  const int64_t per = (rows + want - 1) / want;
-  return make_chunks(n, counts, per < 1 ? 1 : per);
+  const int per_cu = cols > 4096 ? 1 : cols > 2048 ? 2 : cols > 1024 ? 4 : cols > 512 ? 8 : 16;
+  const int64_t want = static_cast<int64_t>(device_cus()) * per_cu;
+  int64_t per = (rows + want - 1) / want;
+  per = per < 2 ? 2 : per;  // the rows that are worked on at a time
+  Chunks c = make_chunks(n, counts, per);
+  while (c.chunk0[n] > want && per < rows) {
+    per += (per + 31) / 32;
+    c = make_chunks(n, counts, per);
+  }
+  return c;
 }
 
 size_t layernorm_backward_bytes(const Chunks& c, int64_t cols) {
@@ -445,7 +557,7 @@ hipError_t enqueue_layernorm_backward(const LayerNormBackward& a, int type, cons
   }
   if (a.dweight || a.dbias)
     launch("sum_chunks", k_sum_chunks,
-           dim3(static_cast<uint32_t>((2 * a.cols + kBlock - 1) / kBlock), c.n), dim3(kBlock), 0,
+           dim3(static_cast<uint32_t>((2 * a.cols + 63) / 64), c.n), dim3(kBlock), 0,
            s, partial, a.cols, c, a.dweight, a.ld_dweight, a.dbias, a.ld_dbias);
   return hipGetLastError();
 }
