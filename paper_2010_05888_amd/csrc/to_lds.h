@@ -13,6 +13,11 @@
 
 namespace garfield {
 
+// The compiler does not look into them either for what must lie between two
+// instructions: a scalar register that a vector instruction has written (a buffer's,
+// say) may be read by a load five wait states later at the earliest, and m0 one after
+// it is set. s_mov and s_nop 3 before every load are five.
+
 typedef __attribute__((address_space(3))) void* LocalPtr;
 
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
@@ -33,15 +38,37 @@ __device__ __forceinline__ u4 buffer_of(const void* p, uint32_t bytes) {
 // 16 bytes a lane, from the lane's offset in the buffer to LDS at to + 16 * lane.
 // `to` is the wave's.
 __device__ __forceinline__ void load_to_lds16(u4 buffer, uint32_t from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(buffer)
                : "memory");
 }
 
+__device__ __forceinline__ void load_to_lds4(u4 buffer, uint32_t from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(buffer)
+               : "memory");
+}
+
+// The same from the lane's address, for offsets beyond 32 bits.
+__device__ __forceinline__ void load_to_lds16(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory");
+}
+
+__device__ __forceinline__ void load_to_lds4(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory");
+}
+
 // One byte a lane, to the low byte of a word of LDS at to + 4 * lane (the others 0).
 __device__ __forceinline__ void load_to_lds1(u4 buffer, uint32_t from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_ubyte %1, %2, 0 offen lds"
                :
                : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(buffer)
                : "memory");

@@ -68,15 +68,20 @@ def _functions():
     return _fn
 
 
+_empty = torch.empty
+_this_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _run(name: str, device: torch.device, *args):
     """Call a function of the library on the device's current stream."""
     fn = _fn.get(name) or _functions()[name]
     i = device.index
-    if i == torch._C._cuda_getDevice():
-        code = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    if i == _this_device():
+        code = fn(*args, _raw_stream(i))
     else:
         with torch.cuda.device(i):
-            code = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+            code = fn(*args, _raw_stream(i))
     if code != OK:
         raise GarfieldError(code, name, load().garfield_strerror(code).decode())
 
@@ -102,7 +107,7 @@ def _matrix(x, name: str, dtype=None):
 
 
 def _vector(v, name: str, length: int, dtypes, device):
-    if (not isinstance(v, torch.Tensor) or v.shape != (length,) or v.dtype not in dtypes
+    if (not isinstance(v, torch.Tensor) or v.dtype not in dtypes or v.shape != (length,)
             or v.device != device or not v.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous 1-D tensor of {length} values of "
                          f"{' or '.join(str(d) for d in dtypes)} on {device}")
@@ -123,7 +128,7 @@ class Checkpoint:
     127). Made by ``checkpoint()`` and ``layernorm()``, or from tensors that hold
     such blocks."""
 
-    __slots__ = ("rows", "cols", "device", "_held", "_flat", "_values", "_exponents")
+    __slots__ = ("rows", "cols", "device", "_held", "_at", "_flat", "_values", "_exponents")
 
     def __init__(self, values: torch.Tensor, exponents: torch.Tensor, cols: int):
         if (not isinstance(values, torch.Tensor) or values.dim() != 2
@@ -148,41 +153,45 @@ class Checkpoint:
         self.rows, self.cols, self.device, self._flat = rows, cols, values.device, None
         self._values, self._exponents = values, exponents
         self._held = _Block8(pv, pe, rows, cols, ldv, lde)
+        self._at = _c.byref(self._held)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Checkpoint":
         """Room for rows x cols values, to be written."""
         width, held = _padded(cols)
+        # rows a multiple of 8 KiB apart share memory channels: a product of 16384 x 8192 with
+        # 8192 x 8192 values takes 960 to 1080 us from such rows and 920 to 930 from these
+        ld = width if width % 8192 or not width else width + BLOCK
         c = cls.__new__(cls)
-        c._flat = flat = torch.empty(rows * (width + held), dtype=torch.uint8, device=device)
+        c._flat = flat = _empty(rows * (ld + held), dtype=torch.uint8, device=device)
         c._values = c._exponents = None
         c.rows, c.cols, c.device = rows, cols, flat.device
         at = flat.data_ptr()
-        c._held = _Block8(at, at + rows * width, rows, cols, width, held)
+        c._held = _Block8(at, at + rows * ld, rows, cols, ld, held)
+        c._at = _c.byref(c._held)
         return c
-
-    def _part(self, width: int, at: int) -> torch.Tensor:
-        return self._flat[at:at + self.rows * width].view(self.rows, width)
 
     @property
     def values(self) -> torch.Tensor:
         if self._values is None:
-            self._values = self._part(_padded(self.cols)[0], 0).view(torch.float8_e4m3fn)
+            self._values = self._flat.view(torch.float8_e4m3fn).as_strided(
+                (self.rows, _padded(self.cols)[0]), (self._held.ld_values, 1))
         return self._values
 
     @property
     def exponents(self) -> torch.Tensor:
         if self._exponents is None:
-            width, held = _padded(self.cols)
-            self._exponents = self._part(held, self.rows * width)
+            held = self._held
+            self._exponents = self._flat.as_strided(
+                (self.rows, held.ld_exponents), (held.ld_exponents, 1), self.rows * held.ld_values)
         return self._exponents
 
     def restore(self, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """The values, rounded once to dtype (bfloat16 and float32 hold them exactly)."""
         if dtype not in TYPES:
             raise ValueError("dtype must be float32, bfloat16 or float16")
-        out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.device)
-        _run("garfield_restore", self.device, self._held, out.data_ptr(), TYPES[dtype],
+        out = _empty((self.rows, self.cols), dtype=dtype, device=self.device)
+        _run("garfield_restore", self.device, self._at, out.data_ptr(), TYPES[dtype],
              max(self.cols, 1))
         return out
 
@@ -193,7 +202,7 @@ def checkpoint(x: torch.Tensor, transposed: bool = False) -> Checkpoint:
     dev = x.device
     c = Checkpoint.empty(cols, rows, dev) if transposed else Checkpoint.empty(rows, cols, dev)
     _run("garfield_checkpoint", dev, x.data_ptr(), kind, rows, cols, ld, 1 if transposed else 0,
-         c._held)
+         c._at)
     return c
 
 
@@ -219,13 +228,15 @@ def layernorm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
     dev, dtype = x.device, x.dtype
     pw = _vector(weight, "weight", cols, _WEIGHTS[dtype], dev)
     pb = None if bias is None else _vector(bias, "bias", cols, (weight.dtype,), dev)
-    out = torch.empty((rows, cols), dtype=dtype, device=dev) if y else None
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    out = None
+    if y:
+        out = torch.empty_like(x) if ld == cols else _empty((rows, cols), dtype=dtype, device=dev)
+    mean, rstd = _empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
     cy = Checkpoint.empty(rows, cols, dev) if y8 else None
     cx = Checkpoint.empty(rows, cols, dev) if x8 else None
     _run("garfield_layernorm", dev, x.data_ptr(), kind, rows, cols, ld, pw, pb,
          TYPES[weight.dtype], eps, out.data_ptr() if y else None, cols, mean.data_ptr(),
-         rstd.data_ptr(), cy._held if y8 else None, cx._held if x8 else None)
+         rstd.data_ptr(), cy._at if y8 else None, cx._at if x8 else None)
     return LayerNorm(out, mean, rstd, cy, cx)
 
 
@@ -260,7 +271,7 @@ def _rows_of_workers(out, name: str, shape, device):
 
 def _workspace(name: str, device, *args):
     need = (_fn.get(name) or _functions()[name])(*args)
-    return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+    return (_empty(need, dtype=torch.uint8, device=device) if need else None), need
 
 
 def layernorm_backward(dy: torch.Tensor, x, mean: torch.Tensor, rstd: torch.Tensor,
@@ -273,7 +284,7 @@ def layernorm_backward(dy: torch.Tensor, x, mean: torch.Tensor, rstd: torch.Tens
     rows, cols, ld, kind = _matrix(dy, "dy")
     dev = dy.device
     if isinstance(x, Checkpoint):
-        px, ldx, x8, shape = None, 0, x._held, (x.rows, x.cols)
+        px, ldx, x8, shape = None, 0, x._at, (x.rows, x.cols)
     else:
         r, c, ldx, _ = _matrix(x, "x", dy.dtype)
         px, x8, shape = x.data_ptr(), None, (r, c)
@@ -285,7 +296,7 @@ def layernorm_backward(dy: torch.Tensor, x, mean: torch.Tensor, rstd: torch.Tens
     n, counts = _counted(counts, rows)
     dweight, ldw = _rows_of_workers(dweight, "dweight", (n, cols), dev)
     dbias, ldb = _rows_of_workers(dbias, "dbias", (n, cols), dev)
-    dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
+    dx = torch.empty_like(dy) if ld == cols else _empty((rows, cols), dtype=dy.dtype, device=dev)
     ws, need = _workspace("garfield_layernorm_backward_workspace", dev, rows, cols, n, counts)
     _run("garfield_layernorm_backward", dev, dy.data_ptr(), kind, rows, cols, ld, px, ldx, x8, pm,
          pr, pw, TYPES[weight.dtype], dx.data_ptr(), cols, n, counts, dweight.data_ptr(), ldw,
@@ -306,9 +317,9 @@ def linear8(x8: Checkpoint, w8: Checkpoint, bias: torch.Tensor | None = None,
     if dtype not in TYPES:
         raise ValueError("dtype must be float32, bfloat16 or float16")
     pb = None if bias is None else _vector(bias, "bias", n, (torch.float32,), dev)
-    out = torch.empty((m, n), dtype=dtype, device=dev)
+    out = _empty((m, n), dtype=dtype, device=dev)
     ws, need = _workspace("garfield_linear8_workspace", dev, m, n, k)
-    _run("garfield_linear8", dev, x8._held, w8._held, pb, 1 if fast else 0, out.data_ptr(),
+    _run("garfield_linear8", dev, x8._at, w8._at, pb, 1 if fast else 0, out.data_ptr(),
          TYPES[dtype], n or 1, ws.data_ptr() if need else None, need)
     return out
 
@@ -333,6 +344,6 @@ def weight_gradient(dy: torch.Tensor, x8: Checkpoint, counts=None,
     py = dy.data_ptr()
     ws, need = _workspace("garfield_weight_gradient_workspace", dev, py, kind, tokens, outputs,
                           x8.cols, ld, n, counts)
-    _run("garfield_weight_gradient", dev, py, kind, tokens, outputs, ld, x8._held, n, counts,
+    _run("garfield_weight_gradient", dev, py, kind, tokens, outputs, ld, x8._at, n, counts,
          out.data_ptr(), ldw, pb, ldb, ws.data_ptr() if need else None, need)
     return out, dbias
