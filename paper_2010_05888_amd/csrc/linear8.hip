@@ -16,6 +16,7 @@
 #include "block8.h"
 #include "internal.h"
 #include "timing.h"
+#include "to_lds.h"
 #include "worker.h"
 
 namespace garfield {
@@ -139,9 +140,6 @@ void choose_few(const garfield_block8& x, const garfield_block8& w, const float*
   else launch_few<T, 4, FB>(x, w, bias, out, ld, s);
 }
 
-typedef __attribute__((address_space(1))) const void* GlobalPtr;
-typedef __attribute__((address_space(3))) void* LocalPtr;
-
 // Workgroup id to tile: workgroups go to the eight XCDs in turn, so an XCD's
 // share is made contiguous, and inside it eight token tiles deep: the tiles that
 // an XCD has in work share their rows of X and W in its L2.
@@ -160,8 +158,11 @@ __device__ __forceinline__ Place place_of(uint32_t id, uint32_t total, uint32_t 
 
 // A workgroup makes a tile of WJ * FA * 16 outputs x WM * FB * 16 tokens, a wave
 // FA x FB products of 16 x 16, block after block of 128 columns. The next
-// block's codes go from memory straight to LDS while the waves work on this one,
-// the exponents of four blocks with every fourth of them.
+// block's codes go from memory straight to LDS while the waves work on this one, a few
+// loads at a time between the products of the first half: a wave that issues all of
+// them first waits for the loads of the others before its first product (889 against
+// 937 us at 16384 x 8192 x 8320), and one that spreads them to the end for the last (940).
+// The exponents of four blocks come with every fourth of them.
 // A row of 128 codes is eight 16-byte chunks, chunk c at c ^ (row / 2 % 8). Lane l
 // takes chunks l / 16 and l / 16 + 4 of its rows. LDS serves 16 lanes of a 16-byte
 // read at a time, from two neighbouring groups of 16 lanes the even quarters of
@@ -174,8 +175,10 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
     garfield_block8 x, garfield_block8 w, const float* __restrict__ bias, T* out, int64_t ld,
     uint32_t tiles_m, uint32_t tiles_j) {
   constexpr int kWaves = WJ * WM, kTileJ = WJ * FA * 16, kTileM = WM * FB * 16;
-  constexpr int kRows = kTileJ + kTileM, kLoads = kRows / 8 / kWaves;  // eight rows a load
-  static_assert(kRows % (8 * kWaves) == 0 && kTileJ % 64 == 0 && kTileM % 64 == 0,
+  constexpr int kRows = kTileJ + kTileM;
+  constexpr int kLoadsJ = kTileJ / 8 / kWaves, kLoads = kRows / 8 / kWaves;  // eight rows each
+  static_assert(kTileJ % (8 * kWaves) == 0 && kTileM % (8 * kWaves) == 0 && kTileJ % 64 == 0 &&
+                    kTileM % 64 == 0,
                 "rows are shared out evenly");
   static_assert(kRows <= 64 * kWaves, "a wave fetches the exponents of 64 rows");
   // codes of two blocks, exponents of two groups of four
@@ -185,45 +188,50 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
   const Place at = place_of(blockIdx.x, gridDim.x, tiles_m, tiles_j);
   const int64_t j0 = at.j * kTileJ, m0 = at.m * kTileM;
 
-  // rows of the tile: W's, then X's; those past the end read the last one again
-  const int left_j = static_cast<int>(w.rows - j0 < kTileJ ? w.rows - j0 : kTileJ) - 1;
-  const int left_m = static_cast<int>(x.rows - m0 < kTileM ? x.rows - m0 : kTileM) - 1;
+  // rows of the tile: the last one's number
+  const int last_j = static_cast<int>(w.rows - j0 < kTileJ ? w.rows - j0 : kTileJ) - 1;
+  const int last_m = static_cast<int>(x.rows - m0 < kTileM ? x.rows - m0 : kTileM) - 1;
   const uint8_t* const w0 = w.values + j0 * w.ld_values;
   const uint8_t* const x0 = x.values + m0 * x.ld_values;
-  Offset from[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const bool of_w = i < kLoads * kTileJ / kRows;
-    int row = (i * kWaves + wave) * 8 + lane / 8 - (of_w ? 0 : kTileJ);
-    const int last = of_w ? left_j : left_m;
-    row = row < last ? row : last;
-    from[i] = static_cast<Offset>(row) * static_cast<Offset>(of_w ? w.ld_values : x.ld_values) +
-              ((lane % 8) ^ ((i * kWaves + wave) * 4 + lane / 16) % 8) * 16;
-  }
-  static_assert(kLoads * kTileJ % kRows == 0, "a load is of W's rows or of X's");
+  const uint32_t base = lds_offset(lds) + wave * 1024;
+  // a load brings eight rows, the next one those 8 * kWaves rows on, with the same
+  // exchange of chunks; what it brings for rows past the end is not used
+  constexpr int kApart = 8 * kWaves;
+  static_assert(kApart % 16 == 0, "the exchange is of 16 rows");
+  const int row = wave * 8 + lane / 8, swapped = ((lane % 8) ^ (row / 2 % 8)) * 16;
+  const Offset from_j = static_cast<Offset>(row) * static_cast<Offset>(w.ld_values) + swapped;
+  const Offset from_m = static_cast<Offset>(row) * static_cast<Offset>(x.ld_values) + swapped;
+  auto fetch = [&](int i, int64_t block, int into) {  // load i of a block
+    const bool of_w = i < kLoadsJ;
+    const int n = (of_w ? i : i - kLoadsJ) * kApart, last = of_w ? last_j : last_m;
+    const int64_t ld_values = of_w ? w.ld_values : x.ld_values;
+    const uint8_t* p = (of_w ? w0 : x0) + block * kBlock8;
+    const uint32_t to = base + into * kCodes + i * kWaves * 1024;
+    if constexpr (sizeof(Offset) == 4) {
+      const uint32_t bytes =
+          last < n ? 0
+                   : static_cast<uint32_t>(last - n) * static_cast<uint32_t>(ld_values) + kBlock8;
+      load_to_lds16(buffer_of(p + n * ld_values, bytes), of_w ? from_j : from_m, to);
+    } else {  // the last row again
+      load_to_lds16(p + (of_w ? from_j : from_m) +
+                        ((row + n < last ? row + n : last) - row) * ld_values,
+                    to);
+    }
+  };
+  // the exponents of the wave's 64 rows
   const uint8_t* e0;
   {
-    int row = wave * 64 + lane;
-    const bool of_w = row < kTileJ;
-    row -= of_w ? 0 : kTileJ;
-    const int last = of_w ? left_j : left_m;
-    row = row < last ? row : last;
-    e0 = of_w ? w.exponents + (j0 + row) * w.ld_exponents
-              : x.exponents + (m0 + row) * x.ld_exponents;
+    int r = wave * 64 + lane;
+    const bool of_w = r < kTileJ;
+    r -= of_w ? 0 : kTileJ;
+    const int last = of_w ? last_j : last_m;
+    r = r < last ? r : last;
+    e0 = of_w ? w.exponents + (j0 + r) * w.ld_exponents : x.exponents + (m0 + r) * x.ld_exponents;
   }
-  auto fetch = [&](int block) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const uint8_t* base = (i < kLoads * kTileJ / kRows ? w0 : x0) + block * int64_t{kBlock8};
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(base + from[i]),
-                                       (LocalPtr)(lds + (block & 1) * kCodes + (i * kWaves + wave) * 1024),
-                                       16, 0, 0);
-    }
+  auto fetch_exponents = [&](int block) {
     if (block % 4 == 0 && wave * 64 < kRows)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(e0 + block),
-                                       (LocalPtr)(lds + 2 * kCodes + (block / 4 & 1) * kExponents +
-                                                  wave * 256),
-                                       4, 0, 0);
+      load_to_lds4(e0 + block,
+                   lds_offset(lds) + 2 * kCodes + (block / 4 & 1) * kExponents + wave * 256);
   };
 
   const int wj = wave / WM, wm = wave % WM;
@@ -237,9 +245,15 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
   const int row0 = lane % 16 * kBlock8, chunk0 = (lane / 16) ^ (lane % 16 / 2);
   const int near0 = row0 + chunk0 * 16, near1 = row0 + (chunk0 ^ 4) * 16;
   uint32_t ew[FA], ex[FB];
-  if (blocks > 0) fetch(0);
+  if (blocks > 0) {
+    fetch_exponents(0);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) fetch(i, 0, 0);
+  }
   for (int b = 0; b < blocks; ++b) {
-    __syncthreads();  // block b is there, and block b - 1 has been read
+    wait_for<0>();
+    barrier();  // block b is there, and block b - 1 has been read
+    const int next = b + 1 < blocks ? b + 1 : b, into = (b + 1) & 1;  // the last one twice
     if (b % 4 == 0) {
       const uint32_t* e = reinterpret_cast<const uint32_t*>(lds + 2 * kCodes +
                                                             (b / 4 & 1) * kExponents) + lane % 16;
@@ -265,10 +279,12 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
 #pragma unroll
       for (int k = 0; k < FB; ++k) xf[k] = read(xt + k * 16 * kBlock8);
       wf[0] = read(wt);
-      if (b + 1 < blocks) fetch(b + 1);
+      if (next > b) fetch_exponents(next);
 #pragma unroll
       for (int i = 0; i < FA; ++i) {
         if (i + 1 < FA) wf[(i + 1) & 1] = read(wt + (i + 1) * 16 * kBlock8);
+#pragma unroll
+        for (int l = i * kLoads * 2 / FA; l < (i + 1) * kLoads * 2 / FA && l < kLoads; ++l) fetch(l, next, into);
 #pragma unroll
         for (int k = 0; k < FB; ++k)
           sum[i][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
@@ -276,9 +292,11 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
       }
     } else {
       // a quarter of the lane's codes at a time
-      if (b + 1 < blocks) fetch(b + 1);
+      if (next > b) fetch_exponents(next);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int l = q * kLoads / 2; l < (q + 1) * kLoads / 2 && l < kLoads; ++l) fetch(l, next, into);
         const int near = (q < 2 ? near0 : near1) + q % 2 * 8;
         bf8 xf[FB];
 #pragma unroll
@@ -296,6 +314,7 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
       }
     }
   }
+  wait_for<0>();  // no load outlives the workgroup's LDS
 #pragma unroll
   for (int k = 0; k < FB; ++k) {
     const int64_t m = m0 + (wm * FB + k) * 16 + lane % 16;
