@@ -136,14 +136,19 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wj = wave % 4, wk = wave / 4;
 
-  // an XCD's share of the tiles is contiguous (workgroups go to the XCDs in turn)
+  // An XCD's share of the tiles is contiguous (workgroups go to the XCDs in turn), and
+  // eight tiles of outputs deep: the 32 that it has in work share their columns of dY and
+  // X in its L2 (8 x 16 + 4 x 8 KB a step, where 32 x 1 would be 520 KB).
   const uint32_t total = gridDim.x, share = total / 8, more = total % 8, xcd = blockIdx.x % 8;
   uint32_t at = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
   const int share_of = at / (tiles_j * tiles_k);  // worker by worker in every split
   const int worker = share_of % tokens.n;
   at %= tiles_j * tiles_k;
-  const int64_t j0 = static_cast<int64_t>(at % tiles_j) * kTileJ;
-  const int block0 = at / tiles_j * WK;
+  constexpr uint32_t kDeep = 8;
+  const uint32_t group = kDeep * tiles_k, deep0 = at / group * kDeep;
+  const uint32_t deep = tiles_j - deep0 < kDeep ? tiles_j - deep0 : kDeep;
+  const int64_t j0 = static_cast<int64_t>(deep0 + at % group % deep) * kTileJ;
+  const int block0 = at % group / deep * WK;
   int64_t first = tokens.first[worker], end = tokens.first[worker + 1];
   const int64_t all = (end - first + kTokens - 1) / kTokens;
   const int64_t most = (all + tokens.splits - 1) / tokens.splits * kTokens;
@@ -186,26 +191,35 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
   const uint8_t* at_x = x.values + first * x.ld_values + static_cast<int64_t>(block0) * kBlock8;
   const uint8_t* at_e = x.exponents + first * x.ld_exponents + block0;
   int64_t left = per_part, parts_left = steps > 0 ? a.parts : 0;
-  auto fetch = [&](int place, int odd) {
-    const bool last = left == 1, none = parts_left <= 0;  // two fetches go past the end
-    const u4 of_y = buffer_of(at_y, none ? 0 : last ? last_y : full_y);
-    const u4 of_x = buffer_of(at_x, none ? 0 : last ? last_x : full_x);
-    const u4 of_e = buffer_of(at_e, none ? 0 : last ? last_e : full_e);
+  // A step's loads, in four parts: dY, X, and its exponents with what the next step needs.
+  auto fetch_part = [&](int part, int place, int odd) {
+    const bool last = left == 1, none = parts_left <= 0;  // fetches go past the end
+    if (part < 2) {
+      const u4 of_y = buffer_of(at_y, none ? 0 : last ? last_y : full_y);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      load_to_lds16(of_y, from[i], base + place * kY + (i * kWaves + wave) * 1024);
-    load_to_lds16(of_x, from_x, base + kAtCodes + odd * kCodes + wave * 1024);
-    load_to_lds1(of_e, from_e, base + kAtExponents + odd * kExponents + wave * 256);
-    at_y += kTokens * a.ld;
-    at_x += kTokens * x.ld_values;
-    at_e += kTokens * x.ld_exponents;
-    if (--left == 0) {
-      left = per_part;
-      --parts_left;
-      at_y += a.next - per_part * kTokens * a.ld;
-      at_x -= per_part * kTokens * x.ld_values;
-      at_e -= per_part * kTokens * x.ld_exponents;
+      for (int i = part * kLoads / 2; i < (part + 1) * kLoads / 2; ++i)
+        load_to_lds16(of_y, from[i], base + place * kY + (i * kWaves + wave) * 1024);
+    } else if (part == 2) {
+      const u4 of_x = buffer_of(at_x, none ? 0 : last ? last_x : full_x);
+      load_to_lds16(of_x, from_x, base + kAtCodes + odd * kCodes + wave * 1024);
+    } else {
+      const u4 of_e = buffer_of(at_e, none ? 0 : last ? last_e : full_e);
+      load_to_lds1(of_e, from_e, base + kAtExponents + odd * kExponents + wave * 256);
+      at_y += kTokens * a.ld;
+      at_x += kTokens * x.ld_values;
+      at_e += kTokens * x.ld_exponents;
+      if (--left == 0) {
+        left = per_part;
+        --parts_left;
+        at_y += a.next - per_part * kTokens * a.ld;
+        at_x -= per_part * kTokens * x.ld_values;
+        at_e -= per_part * kTokens * x.ld_exponents;
+      }
     }
+  };
+  auto fetch = [&](int place, int odd) {
+#pragma unroll
+    for (int part = 0; part < 4; ++part) fetch_part(part, place, odd);
   };
   // the thread's own codes, as its wave has fetched them
   struct Codes {
@@ -294,10 +308,10 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
     for (int64_t s = 0; s < steps; ++s) {
       const int of_y = s & 3, odd = s & 1;
       const int next_x = of_x == 2 ? 0 : of_x + 1, after_x = next_x == 2 ? 0 : next_x + 1;
-      fetch((of_y + 3) & 3, 1 - odd);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         read_x(i + 2, of_x);
+        fetch_part(i, (of_y + 3) & 3, 1 - odd);
         multiply(i);
       }
       wait_for<kFetches>();  // step s + 2 is there

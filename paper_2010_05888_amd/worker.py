@@ -242,7 +242,7 @@ def layernorm(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None =
 
 def _counted(counts, rows: int):
     """The workers' tokens as a C array (None: one worker)."""
-    counts = [rows] if counts is None else list(counts)
+    counts = [rows] if counts is None else [int(c) for c in counts]
     if not counts or sum(counts) != rows or min(counts) < 0:
         raise ValueError(f"counts must be the workers' tokens, adding up to {rows}")
     return len(counts), (_i64 * len(counts))(*counts)
