@@ -8,6 +8,8 @@
 // normal values: 1.2e-5 of the result's size off, 7e-5 with wider spreads).
 // Otherwise: codes times 2^s are exact in bf16, and four bf16 instructions of half
 // the rate add the same products with fp32 sums.
+// 16384 x 8192 x 8320: 889 us (2.5 PFLOP/s) fast, 1550 us (1.44) with fp32 sums; the card's
+// power bounds both (zeros: 849 and 1530 us), and the loads' way to LDS the first.
 //
 // W is the instructions' first operand (its rows are the result's rows), so a
 // lane ends with four neighbouring outputs of one token. Lane l gives row
@@ -54,7 +56,8 @@ __device__ __forceinline__ void store_outputs(T* out, const float* bias, int64_t
   }
 }
 
-// Few tokens (up to 16 * FB): the time is W's bytes. A workgroup takes 16 outputs,
+// Few tokens (up to 16 * FB): the time is W's bytes, or latency where they are few
+// (one token, 4096 x 4096: 7.0 us, 2.4 TB/s). A workgroup takes 16 outputs,
 // its waves every WAVES-th block each, operands straight from memory and several
 // blocks at a time; the waves' sums meet in LDS, added in one order. Products are
 // bf16's: the matrix instructions are idle most of the time either way.

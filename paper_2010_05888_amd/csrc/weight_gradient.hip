@@ -6,9 +6,13 @@
 // Both operands have the tokens, over which the sum runs, as rows: LDS holds them
 // as they lie in memory and transposing reads give the matrix instruction its
 // columns. A tile of dw takes 128 inputs, so one block of X and one exponent a
-// token: X goes through registers, where its codes become bf16 once for all the
-// waves; dY goes straight to LDS. Two workgroups share a CU, so that one's
-// products cover the other's stores: dw is 4 bytes for 2 tokens operations.
+// token: X's codes become bf16 in LDS once for all the waves; dY goes straight
+// there.
+//
+// Bounds: the matrix cores' bf16 rate for many tokens a worker (one worker's 16384 x
+// 4096 x 4096: 465 us, 1180 TFLOP/s), the stores of dw, 4 bytes for 2 * tokens operations,
+// for few (19 workers without tokens: 225 us, 5.6 TB/s); 19 workers' 16384 tokens take 705 us,
+// nearly their sum.
 
 #include "block8.h"
 #include "internal.h"
@@ -52,7 +56,7 @@ constexpr int parts_of() {
 }
 int parts_of_type(int type) { return type == GARFIELD_F32 ? 3 : type == GARFIELD_F16 ? 2 : 1; }
 
-// dY as k_weight_gradient reads it: its parts, one matrix after the other, rows
+// dY as k_weight_gradient reads it (5.3 us for 1000 x 1001 in fp32): its parts, one matrix after the other, rows
 // of a multiple of eight columns (the last ones 0).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_pack(const T* __restrict__ dy, int64_t tokens,
@@ -375,7 +379,8 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
 }
 
 // The splits' gradients added in ascending order: sums of `length` values for each of
-// n workers, `next` values apart in partial (n * next for each split).
+// n workers, `next` values apart in partial (n * next for each split). A pass over
+// memory; its bytes are part of plan_gradient's choice.
 __global__ __launch_bounds__(kBlock) void k_sum_splits(const float* __restrict__ partial,
                                                        int64_t length, int64_t next, int n,
                                                        int splits, float* __restrict__ out,
@@ -431,16 +436,17 @@ struct Plan {
 
 // A round of workgroups costs about their time alone on a CU, which for a step of 32
 // tokens is, in units of the largest tile's: 256 x 256, one a CU, 1; two of 128 x 128 on
-// a CU 0.73 (measured at 16384 x 4096 x 4096: 491 us one round, 718 us two); three of 64 x 128
-// 0.6. Few tiles of many tokens leave CUs idle: their tokens are cut into up to 16
-// shares of at least eight steps, whose sums cost a pass over splits * 4 bytes for
-// each value of dw (as long as some 8 steps).
+// a CU 0.72; three of 64 x 128 0.68 (a round of 512 steps at 16384 x 4096 x 4096 on one card:
+// 574, 411 and 388 us). Few tiles of many tokens leave CUs idle: their tokens are cut
+// into up to 16 shares of at least eight steps, whose sums cost a pass over splits * 4
+// bytes for each value of dw (as long as some 8 steps): one worker's 16384 x 2048 x 4096
+// takes 282 us so, and 464, 383 or 582 us uncut in the three forms.
 Plan plan_gradient(int parts, int64_t tokens, int64_t outputs, int64_t inputs, int n) {
   struct Shape {
     int wk, fb, slots;
     double time;
   };
-  static constexpr Shape kShapes[] = {{2, 4, 1, 1.0}, {1, 2, 2, 0.73}, {1, 1, 3, 0.6}};
+  static constexpr Shape kShapes[] = {{2, 4, 1, 1.0}, {1, 2, 2, 0.72}, {1, 1, 3, 0.68}};
   const int cus = device_cus();
   const double steps = static_cast<double>((tokens / n + kTokens) / kTokens) * parts;
   Plan best = {1, 1, 1};

@@ -12,6 +12,9 @@ rules take:
     dx, _, _ = layernorm_backward(dy, r.x8, r.mean, r.rstd, weight, counts, dweight=..., dbias=...)
     aggregate, sel = gar("multikrum", grads, f)
 
+Nothing here takes part in torch's autograd: a backward pass is called like a
+forward pass.
+
 Thin binding over the C-ABI of ``include/garfield_worker.h``, whose kernels do
 all the computing; calls run on the current stream of their tensors' device and
 share no scratch, so calls on several streams may overlap.
