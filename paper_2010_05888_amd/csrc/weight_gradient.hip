@@ -14,6 +14,8 @@
 // for few (19 workers without tokens: 225 us, 5.6 TB/s); 19 workers' 16384 tokens take 705 us,
 // nearly their sum.
 
+#include <type_traits>
+
 #include "block8.h"
 #include "internal.h"
 #include "timing.h"
@@ -126,7 +128,7 @@ template <int WK, int FB>
 __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
     Parts a, garfield_block8 x, Tokens tokens, float* __restrict__ dw, int64_t ld_dw,
     float* __restrict__ dbias, int64_t ld_dbias, int64_t outputs, uint32_t tiles_j,
-    uint32_t tiles_k) {
+    uint32_t tiles_k, bool whole_lines) {
   constexpr int kFA = 8, kWaves = 4 * WK, kTileJ = 64 * FB, kTileK = 128 * WK;
   constexpr int kRowJ = kTileJ * 2, kRowK = kTileK * 2;  // bytes
   constexpr int kY = kTokens * kRowJ, kX = kTokens * kRowK, kCodes = kTokens * kTileK;
@@ -351,31 +353,41 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
   uint8_t* const own = lds + wave * 16 * kRow;
   const int64_t k0 = static_cast<int64_t>(block0 + wk) * kBlock8 + lane % 32 * 4;
   const int64_t left_k = x.cols - k0;
+  // Whole lines go past the caches (3% at 19 workers, 16384 x 4096 x 4096); parts of
+  // lines stay for their other parts (11 workers, 500 x 2001 x 1999: 48 us, and 72 past them).
+  auto store = [&](auto past_caches) {
 #pragma unroll
-  for (int k = 0; k < FB; ++k) {
-    const int64_t j = j0 + (wj * FB + k) * 16;
-    if (with_bias && lane < 16 && j + lane < outputs) dbias[share_of * ld_dbias + j + lane] = ones[k][0];
+    for (int k = 0; k < FB; ++k) {
+      const int64_t j = j0 + (wj * FB + k) * 16;
+      if (with_bias && lane < 16 && j + lane < outputs)
+        dbias[share_of * ld_dbias + j + lane] = ones[k][0];
 #pragma unroll
-    for (int i = 0; i < kFA; ++i)
-      *reinterpret_cast<v4f*>(own + lane % 16 * kRow + i * 64 + lane / 16 * 16) = sum[i][k];
+      for (int i = 0; i < kFA; ++i)
+        *reinterpret_cast<v4f*>(own + lane % 16 * kRow + i * 64 + lane / 16 * 16) = sum[i][k];
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      const int row = r + lane / 32;
-      const v4f t = *reinterpret_cast<const v4f*>(own + row * kRow + lane % 32 * 16);
-      if (j + row >= outputs) continue;
-      float* to = dw + share_of * ld_dw + (j + row) * x.cols + k0;
-      if (left_k >= 4) {
-        Four v;
+      for (int r = 0; r < 16; r += 2) {
+        const int row = r + lane / 32;
+        const v4f t = *reinterpret_cast<const v4f*>(own + row * kRow + lane % 32 * 16);
+        if (j + row >= outputs) continue;
+        float* to = dw + share_of * ld_dw + (j + row) * x.cols + k0;
+        if (left_k >= 4) {
+          Four v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = t[e];
-        __builtin_nontemporal_store(v, reinterpret_cast<Four*>(to));
-      } else {
+          for (int e = 0; e < 4; ++e) v[e] = t[e];
+          if constexpr (decltype(past_caches)::value)
+            __builtin_nontemporal_store(v, reinterpret_cast<Four*>(to));
+          else
+            *reinterpret_cast<Four*>(to) = v;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < left_k) to[e] = t[e];
+          for (int e = 0; e < 4; ++e)
+            if (e < left_k) to[e] = t[e];
+        }
       }
     }
-  }
+  };
+  if (whole_lines) store(std::true_type());
+  else store(std::false_type());
 }
 
 // The splits' gradients added in ascending order: sums of `length` values for each of
@@ -474,9 +486,12 @@ void launch_gradient(const Parts& p, const WeightGradient& a, const Tokens& toke
                      int64_t ld_dw, float* dbias, int64_t ld_dbias, hipStream_t s) {
   const uint32_t tiles_j = static_cast<uint32_t>((a.outputs + 64 * FB - 1) / (64 * FB));
   const uint32_t tiles_k = static_cast<uint32_t>((a.x.cols + 128 * WK - 1) / (128 * WK));
+  // whether tiles' rows are whole lines of 128 bytes
+  const bool whole_lines = reinterpret_cast<uintptr_t>(dw) % 128 == 0 && ld_dw % 32 == 0 &&
+                           a.x.cols % 32 == 0;
   launch("weight_gradient", k_weight_gradient<WK, FB>,
          dim3(tiles_j * tiles_k * tokens.n * tokens.splits), dim3(256 * WK), 0, s, p, a.x, tokens,
-         dw, ld_dw, dbias, ld_dbias, a.outputs, tiles_j, tiles_k);
+         dw, ld_dw, dbias, ld_dbias, a.outputs, tiles_j, tiles_k, whole_lines);
 }
 
 void launch_sums(const float* partial, int64_t length, int64_t next, const Tokens& tokens,
