@@ -135,6 +135,7 @@ void launch_few(const garfield_block8& x, const garfield_block8& w, const float*
          dim3(64 * WAVES), 0, s, x, w, bias, static_cast<T*>(out), ld);
 }
 
+// As many waves as there are blocks for, up to 16.
 template <typename T, int FB>
 void choose_few(const garfield_block8& x, const garfield_block8& w, const float* bias, void* out,
                 int64_t ld, hipStream_t s) {
@@ -172,10 +173,8 @@ __device__ __forceinline__ Place place_of(uint32_t id, uint32_t total, uint32_t 
 // The exponents of four blocks come with every fourth of them.
 // A row of 128 codes is eight 16-byte chunks, chunk c at c ^ (row / 2 % 8). Lane l
 // takes chunks l / 16 and l / 16 + 4 of its rows. LDS serves 16 lanes of a 16-byte
-// read at a time, from two neighbouring groups of 16 lanes the even quarters of
-// one and the odd ones of the other; two rows are the banks' 256 bytes, and so each
-// lane reads banks of its own. Lane l takes chunks
-// 2 (l / 16) and 2 (l / 16) + 1 of its rows.
+// read at a time: lanes 0-3 and 12-15 with 20-27, then 4-11 with 16-19 and 28-31. Two rows
+// are the banks' 256 bytes, and so each lane reads banks of its own.
 // Offset: of a row from its tile's first one.
 template <typename T, bool FAST, typename Offset, int WJ, int WM, int FA, int FB>
 __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
@@ -300,7 +299,8 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
       for (int i = 0; i < FA; ++i) {
         if (i + 1 < FA) wf[(i + 1) & 1] = read(wt + (i + 1) * 16 * kBlock8);
 #pragma unroll
-        for (int l = i * kLoads * 2 / FA; l < (i + 1) * kLoads * 2 / FA && l < kLoads; ++l) fetch(l, next, into);
+        for (int l = i * kLoads * 2 / FA; l < (i + 1) * kLoads * 2 / FA && l < kLoads; ++l)
+          fetch(l, next, into);
 #pragma unroll
         for (int k = 0; k < FB; ++k)
           sum[i][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
@@ -312,7 +312,8 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_linear8_tile(
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
 #pragma unroll
-        for (int l = q * kLoads / 2; l < (q + 1) * kLoads / 2 && l < kLoads; ++l) fetch(l, next, into);
+        for (int l = q * kLoads / 2; l < (q + 1) * kLoads / 2 && l < kLoads; ++l)
+          fetch(l, next, into);
         const int near = (q < 2 ? near0 : near1) + q % 2 * 8;
         bf8 xf[FB];
 #pragma unroll
@@ -377,7 +378,7 @@ Shares plan_shares(int64_t tokens, int64_t outputs, int64_t inputs) {
   const int blocks = static_cast<int>((inputs + kBlock8 - 1) / kBlock8);
   Shares s = {1, blocks, (outputs + 3) / 4 * 4};
   const int64_t small = tiles_of(tokens, outputs, 64), most = 3 * int64_t{device_cus()};
-  if (tokens <= 64 || outputs == 0 || 2 * small > device_cus()) return s;
+  if (tokens <= 32 || outputs == 0 || 2 * small > device_cus()) return s;
   const int64_t want = most / small < blocks / 4 ? most / small : blocks / 4;
   if (want < 2) return s;
   const int per = static_cast<int>((blocks + want - 1) / want + 3) / 4 * 4;
@@ -397,6 +398,10 @@ void launch_tile(const garfield_block8& x, const garfield_block8& w, const float
          static_cast<T*>(out), ld, tiles_m, tiles_j, p.blocks);
 }
 
+// The largest tile of which there are 192 (of 256 CUs): 3500 x 3500 x 2000, 196 tiles of 256 x
+// 256, takes 34 us (55 with fp32 sums), 41 (65) in tiles of 128 and 49 (66) in tiles of 64;
+// 2000^3, 256 of 128 x 128, 17.6 (24.9), against 29.7 (49.3) and 17.1 (25.2); 777 x 1000 x 1500 in
+// tiles of 64 7.8 (10.0), of 128 12.8 (18.1).
 template <typename T, bool FAST>
 void choose_tile(const garfield_block8& x, const garfield_block8& w, const float* bias, void* out,
                  int64_t ld, const Shares& p, hipStream_t s) {
@@ -410,13 +415,16 @@ void choose_tile(const garfield_block8& x, const garfield_block8& w, const float
     launch_tile<T, FAST, uint32_t, 2, 2, 2, 2>(x, w, bias, out, ld, p, s);
 }
 
+// Up to 32 tokens the form for few (4096 x 4096: 16 tokens 8.0 us, 32 10.6; 11.2 and 11.0 in
+// tiles with shares).
 template <typename T>
 void choose_linear8(const garfield_block8& x, const garfield_block8& w, const float* bias,
                     bool fast, void* out, int64_t ld, float* partial, hipStream_t s) {
   if (x.rows <= 16) return choose_few<T, 1>(x, w, bias, out, ld, s);
   if (x.rows <= 32) return choose_few<T, 2>(x, w, bias, out, ld, s);
-  if (x.rows <= 64) return choose_few<T, 4>(x, w, bias, out, ld, s);
   const Shares p = plan_shares(x.rows, w.rows, x.cols);
+  // up to 64 tokens: 64 x 4096 x 4096 takes 15.8 us so, and 12.3 in tiles with shares
+  if (x.rows <= 64 && p.count == 1) return choose_few<T, 4>(x, w, bias, out, ld, s);
   if (p.count > 1) {
     if (fast) choose_tile<float, true>(x, w, nullptr, partial, p.ld, p, s);
     else choose_tile<float, false>(x, w, nullptr, partial, p.ld, p, s);

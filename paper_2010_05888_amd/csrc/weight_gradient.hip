@@ -5,8 +5,8 @@
 //
 // Both operands have the tokens, over which the sum runs, as rows: LDS holds them
 // as they lie in memory and transposing reads give the matrix instruction its
-// columns. A tile of dw takes 128 inputs, so one block of X and one exponent a
-// token: X's codes become bf16 in LDS once for all the waves; dY goes straight
+// columns. A wave's part of dw is 128 inputs wide, one block of X with one exponent
+// a token: X's codes become bf16 in LDS once for all the waves; dY goes straight
 // there.
 //
 // Bounds: the matrix cores' bf16 rate for many tokens a worker (one worker's 16384 x
@@ -58,8 +58,8 @@ constexpr int parts_of() {
 }
 int parts_of_type(int type) { return type == GARFIELD_F32 ? 3 : type == GARFIELD_F16 ? 2 : 1; }
 
-// dY as k_weight_gradient reads it (5.3 us for 1000 x 1001 in fp32): its parts, one matrix after the other, rows
-// of a multiple of eight columns (the last ones 0).
+// dY as k_weight_gradient reads it (5.3 us for 1000 x 1001 in fp32): its parts, one
+// matrix after the other, rows of a multiple of eight columns (the last ones 0).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_pack(const T* __restrict__ dy, int64_t tokens,
                                                  int64_t outputs, int64_t lddy, int64_t vectors,
