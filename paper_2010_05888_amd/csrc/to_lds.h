@@ -44,14 +44,7 @@ __device__ __forceinline__ void load_to_lds16(u4 buffer, uint32_t from, uint32_t
                : "memory");
 }
 
-__device__ __forceinline__ void load_to_lds4(u4 buffer, uint32_t from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               :
-               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from), "s"(buffer)
-               : "memory");
-}
-
-// The same from the lane's address, for offsets beyond 32 bits.
+// 16 and 4 bytes a lane from the lane's address.
 __device__ __forceinline__ void load_to_lds16(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off"
                :
