@@ -62,12 +62,13 @@ _fn = {}
 
 
 def _functions():
+    global _fn
     if not _fn:
-        lib = load()
+        lib, table = load(), {}
         for name, (restype, argtypes) in _SIGNATURES.items():
-            fn = getattr(lib, name)
+            table[name] = fn = getattr(lib, name)
             fn.restype, fn.argtypes = restype, argtypes
-            _fn[name] = fn
+        _fn = table  # only when whole: another thread may be here
     return _fn
 
 
