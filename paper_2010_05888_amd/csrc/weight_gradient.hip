@@ -489,9 +489,20 @@ void launch_gradient(const Parts& p, const WeightGradient& a, const Tokens& toke
   // whether tiles' rows are whole lines of 128 bytes
   const bool whole_lines = reinterpret_cast<uintptr_t>(dw) % 128 == 0 && ld_dw % 32 == 0 &&
                            a.x.cols % 32 == 0;
-  launch("weight_gradient", k_weight_gradient<WK, FB>,
-         dim3(tiles_j * tiles_k * tokens.n * tokens.splits), dim3(256 * WK), 0, s, p, a.x, tokens,
-         dw, ld_dw, dbias, ld_dbias, a.outputs, tiles_j, tiles_k, whole_lines);
+  // A launch has fewer than 2^32 threads. Few outputs of many inputs and workers have more
+  // tiles (one worker's always fit, and tokens in shares are few tiles' only): the workers
+  // then take several launches.
+  const int64_t tiles = int64_t{tiles_j} * tiles_k * tokens.splits;
+  const int fit = static_cast<int>(0xffffffff / (256 * WK) / tiles);
+  for (int w = 0; w < tokens.n; w += fit) {
+    Tokens some = tokens;
+    some.n = tokens.n - w < fit ? tokens.n - w : fit;
+    for (int i = 0; i <= some.n; ++i) some.first[i] = tokens.first[w + i];
+    launch("weight_gradient", k_weight_gradient<WK, FB>,
+           dim3(static_cast<uint32_t>(tiles * some.n)), dim3(256 * WK), 0, s, p, a.x, some,
+           dw + w * ld_dw, ld_dw, dbias ? dbias + w * ld_dbias : nullptr, ld_dbias, a.outputs,
+           tiles_j, tiles_k, whole_lines);
+  }
 }
 
 void launch_sums(const float* partial, int64_t length, int64_t next, const Tokens& tokens,
