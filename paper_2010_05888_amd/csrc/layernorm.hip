@@ -456,8 +456,8 @@ __global__ __launch_bounds__(64) void k_layernorm_dw_long(LayerNormBackward a, C
   store8_upto(out + a.cols + c, a.cols - c, db);
 }
 
-// The chunks of a worker added in one order: column blockIdx.x * 64 + threadIdx.x % 64 of
-// partial[chunk][2][cols] for worker blockIdx.y, every fourth chunk to a wave.
+// The chunks of a worker added in one order: 64 columns of partial[chunk][2][cols] at a
+// time for worker blockIdx.y, every fourth chunk to a wave.
 __global__ __launch_bounds__(kBlock) void k_sum_chunks(const float* __restrict__ partial,
                                                        int64_t cols, Chunks chunks,
                                                        float* __restrict__ dweight,
@@ -465,23 +465,27 @@ __global__ __launch_bounds__(kBlock) void k_sum_chunks(const float* __restrict__
                                                        float* __restrict__ dbias,
                                                        int64_t ld_dbias) {
   __shared__ float sums[4][64];
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x % 64;
-  const int worker = blockIdx.y, part = threadIdx.x / 64;
-  float sum = 0.0f;
-  if (i < 2 * cols) {
+  const int lane = threadIdx.x % 64, part = threadIdx.x / 64, worker = blockIdx.y;
+  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * 64; i0 < 2 * cols;
+       i0 += static_cast<int64_t>(gridDim.x) * 64) {
+    const int64_t i = i0 + lane;
+    float sum = 0.0f;
+    if (i < 2 * cols) {
 #pragma unroll 8
-    for (int c = chunks.chunk0[worker] + part; c < chunks.chunk0[worker + 1]; c += 4)
-      sum += partial[static_cast<int64_t>(c) * 2 * cols + i];
-  }
-  sums[part][threadIdx.x % 64] = sum;
-  __syncthreads();
-  if (part > 0 || i >= 2 * cols) return;
-  sum = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) +
-        (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
-  if (i < cols) {
-    if (dweight) dweight[worker * ld_dweight + i] = sum;
-  } else if (dbias) {
-    dbias[worker * ld_dbias + i - cols] = sum;
+      for (int c = chunks.chunk0[worker] + part; c < chunks.chunk0[worker + 1]; c += 4)
+        sum += partial[static_cast<int64_t>(c) * 2 * cols + i];
+    }
+    sums[part][lane] = sum;
+    __syncthreads();
+    if (part == 0 && i < 2 * cols) {
+      sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+      if (i < cols) {
+        if (dweight) dweight[worker * ld_dweight + i] = sum;
+      } else if (dbias) {
+        dbias[worker * ld_dbias + i - cols] = sum;
+      }
+    }
+    __syncthreads();  // the sums' places are free
   }
 }
 
@@ -559,10 +563,13 @@ hipError_t enqueue_layernorm_backward(const LayerNormBackward& a, int type, cons
     else if (type == GARFIELD_BF16) choose_x<__bf16>(a, c, partial, s);
     else choose_x<_Float16>(a, c, partial, s);
   }
-  if (a.dweight || a.dbias)
+  if (a.dweight || a.dbias) {
+    // a workgroup for 64 columns, up to 2^23 of them: a launch has fewer than 2^32 threads
+    const int64_t groups = (2 * a.cols + 63) / 64, most = int64_t{1} << 23;
     launch("sum_chunks", k_sum_chunks,
-           dim3(static_cast<uint32_t>((2 * a.cols + 63) / 64), c.n), dim3(kBlock), 0,
-           s, partial, a.cols, c, a.dweight, a.ld_dweight, a.dbias, a.ld_dbias);
+           dim3(static_cast<uint32_t>(groups < most ? groups : most), c.n), dim3(kBlock), 0, s,
+           partial, a.cols, c, a.dweight, a.ld_dweight, a.dbias, a.ld_dbias);
+  }
   return hipGetLastError();
 }
 

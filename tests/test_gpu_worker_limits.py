@@ -37,3 +37,34 @@ def test_weight_gradient_of_more_tiles_than_a_launch_takes():
         assert bool(((dw[w].double() - d.T @ v).abs() <= bound).all()), w
         assert abs(float(dbias[w, 0]) - float(d.sum())) <= 2 * (counts[w] + 4) * U * float(
             d.abs().sum()) + 1e-40, w
+
+
+def test_layernorm_backward_of_rows_wider_than_a_launch_of_sums():
+    """2^29 + 65 columns: with a workgroup for 64 columns of dweight and dbias, their sums would take
+    2^24 + 3 workgroups of 256 threads. A row's own sums: a lane adds cols / 1024 terms."""
+    cols, counts = (1 << 29) + 65, [1, 0, 1]
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    dy = torch.randn(2, cols, device=DEV, generator=gen, dtype=BF16)
+    x = torch.randn(2, cols, device=DEV, generator=gen, dtype=BF16)
+    mean, rstd = torch.tensor([0.25, -0.5], device=DEV), torch.tensor([1.5, 0.75], device=DEV)
+    weight = torch.full((cols,), 0.5, device=DEV)
+    dx, dw, db = gf.layernorm_backward(dy, x, mean, rstd, weight, counts)
+    step = 1 << 26
+    parts = [slice(a, min(cols, a + step)) for a in range(0, cols, step)]
+    for row, worker in ((0, 0), (1, 2)):
+        m, r = mean[row].double(), rstd[row].double()
+        along = across = size = 0.0
+        for p in parts:
+            g, h = dy[row, p].double() * 0.5, (x[row, p].double() - m) * r
+            along, across = along + float(g.sum()), across + float((g * h).sum())
+            size += float((g * h).abs().sum() + g.abs().sum())
+            want = dy[row, p].double() * h
+            assert bool(((dw[worker, p].double() - want).abs() <= 8 * U * want.abs()).all())
+            assert torch.equal(db[worker, p], dy[row, p].float())
+        for p in parts:
+            g, h = dy[row, p].double() * 0.5, (x[row, p].double() - m) * r
+            want = r * (g - along / cols - h * across / cols)
+            bound = r * ((cols / 1024 + 20) * U * (size / cols) * (1 + h.abs()) + 8 * U * g.abs())
+            bound = bound + (want.abs() + bound) * 2.0 ** -8
+            assert bool(((dx[row, p].double() - want).abs() <= bound).all())
+    assert not bool(dw[1].any()) and not bool(db[1].any())
