@@ -90,7 +90,8 @@ garfield_status garfield_restore(const garfield_block8* c, void* out, int type, 
  * NULL). mean, rstd: rows fp32 values each. y (of `type`), y8 and x8 may be
  * NULL each: y8 is the checkpoint of y's values in 32 bits (before they are
  * rounded to `type`), x8 that of x. Statistics and y are formed in fp32, the
- * variance from the differences to the mean.
+ * variance from the differences to the mean; the mean's sum is kept in fp64 but
+ * for differences within a row, so a row of equal values has exactly that mean.
  */
 garfield_status garfield_layernorm(const void* x, int type, int64_t rows, int64_t cols,
                                    int64_t ldx, const void* weight, const void* bias, int wtype,

@@ -34,6 +34,7 @@ struct LayerNorm {
   int64_t ldx;
   bool weight_f32;  // weight and bias are fp32; else of x's type
   float eps;
+  double share;  // 1 / cols
   void* y;
   int64_t ldy;
   float *mean, *rstd;

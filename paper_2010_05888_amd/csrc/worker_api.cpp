@@ -135,6 +135,7 @@ garfield_status garfield_layernorm(const void* x, int type, int64_t rows, int64_
   a.ldx = ldx;
   a.weight_f32 = wtype == GARFIELD_F32;
   a.eps = eps;
+  a.share = 1.0 / static_cast<double>(cols);
   a.y = y;
   a.ldy = ldy;
   a.mean = mean;
