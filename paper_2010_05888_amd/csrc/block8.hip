@@ -1,7 +1,7 @@
 // 8-bit checkpoints: making them, from a matrix or its transpose, and giving
 // the values back. All are bound by memory: at 8192 x 8192 in bf16 the transposed one takes
 // 50 us (4.0 TB/s: lines of 128 bytes of 128 rows), giving back 30 us (6.7 TB/s); 16384 x
-// 8192 in bf16 to 8 bits 73 us (5.5 TB/s).
+// 8192 in bf16 to 8 bits 71 to 79 us (5.7 to 5.1 TB/s).
 
 #include "block8.h"
 #include "internal.h"

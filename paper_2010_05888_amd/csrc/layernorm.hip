@@ -2,11 +2,10 @@
 // worker.
 //
 // Both read a row once and keep it in registers: the mean, then the variance
-// from the differences to it, then the outputs. Sums are fp32, the mean's across lanes fp64.
-// A lane holds
-// eight neighbouring columns at a time, so the 16 lanes of a DPP row hold one
-// 8-bit block and its largest magnitude needs no memory. Long inputs are bound by
-// memory (a copy runs at 4.7 TB/s, read and written), short ones by latency.
+// from the differences to it, then the outputs. Sums are fp32, the mean's across lanes
+// fp64. A lane holds eight neighbouring columns at a time, so the 16 lanes of a DPP row
+// hold one 8-bit block and its largest magnitude needs no memory. Long inputs are bound
+// by memory (a copy runs at 4.7 TB/s, read and written), short ones by latency.
 
 #include "block8.h"
 #include "internal.h"
@@ -66,9 +65,9 @@ __device__ __forceinline__ void sums_group(F* v, F (*at)[R]) {
 // What a lane adds up for the mean: the differences to its own first value, which are exact
 // or nearly so where a row lies far from 0, and that value as often in fp64. An error of
 // the mean is one of every value of the row: with plain fp32 sums a row of equal values
-// -9999.9 had results up to 0.3 instead of 0. (8192 x 2048 in bf16 with y8 takes 18.3 us so and
-// 17.4 with those, 65536 x 4096 205 and 200.) The first value is taken as 0 if it is not
-// finite, or so large that a difference could be infinite.
+// -9999.9 had results up to 0.3 instead of 0. (8192 x 2048 in bf16 with y8 takes 18.2 us so and
+// 17.7 with those, 65536 x 4096 197 and 196, 8192 x 16384 137 and 132.) The first value is
+// taken as 0 if it is not finite, or so large that a difference could be infinite.
 __device__ __forceinline__ float first_value(float v) {
   return __builtin_fabsf(v) < 0x1p102f ? v : 0.0f;
 }
@@ -98,7 +97,7 @@ __device__ __forceinline__ void store_blocks(const garfield_block8& out, int64_t
     out.exponents[row * out.ld_exponents + b] = static_cast<uint8_t>(b < blocks ? s + 127 : 127);
 }
 
-// A row of 4096 columns in bf16 takes 3.0 us, 65536 of them with x8 280 us (4.8 TB/s).
+// A row of 4096 columns in bf16 takes 3.2 us, 65536 of them with x8 280 us (4.8 TB/s).
 // Rows of up to 512 * WAVES * NV columns, R rows at a time to a team of WAVES waves,
 // NV vectors of eight of each to a lane. Workgroups of four waves hold 4 / WAVES
 // teams. Several rows at a time share what is read of weight and bias, which is
@@ -264,8 +263,9 @@ void launch_layernorm(const LayerNorm& a, hipStream_t s) {
 }
 
 // With many rows two at a time share the reads of weight and bias and the barriers:
-// 65536 x 4096 in bf16 takes 212 us (5.1 TB/s, a copy's rate), one at a time 242, four
-// 218, and a wave to a row of its own 211, but 74 against 67 at 32768 x 2048 with y8.
+// 65536 x 4096 in bf16 takes 200 us (5.4 TB/s, a copy's rate), one at a time 235; 32768 x 2048
+// with y8 67, one at a time 76. (With plain fp32 sums in the mean, 212 us: four rows at a
+// time 218, a wave to a row of its own 211, but 74 against 67 at 32768 x 2048 with y8.)
 template <typename T>
 void choose_layernorm(const LayerNorm& a, hipStream_t s) {
   const bool many = a.rows >= 8 * device_cus();
@@ -428,7 +428,9 @@ __global__ __launch_bounds__(THREADS) void k_layernorm_backward(LayerNormBackwar
   }
 }
 
-// Longer rows: dx from two reads of the row, the weight's gradient by columns.
+// Longer rows: dx from two reads of the row, the weight's gradient by columns, a third.
+// 8192 x 16384 of 19 workers in bf16, x in 8 bits: 188 us for dx, 87 for the chunks' sums and 13
+// for the workers', 2.3 TB/s of what a single read would take.
 template <typename T, bool X8>
 __global__ __launch_bounds__(1024) void k_layernorm_dx_long(LayerNormBackward a) {
   constexpr int kThreads = 1024;

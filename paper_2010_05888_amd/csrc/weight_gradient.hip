@@ -10,9 +10,9 @@
 // there.
 //
 // Bounds: the matrix cores' bf16 rate for many tokens a worker (one worker's 16384 x
-// 4096 x 4096: 465 us, 1180 TFLOP/s), the stores of dw, 4 bytes for 2 * tokens operations,
-// for few (19 workers without tokens: 225 us, 5.6 TB/s); 19 workers' 16384 tokens take 705 us,
-// nearly their sum.
+// 4096 x 4096: 490 us, 1120 TFLOP/s), the stores of dw, 4 bytes for 2 * tokens operations,
+// for few (19 workers without tokens: 229 us, 5.6 TB/s); 19 workers' 16384 tokens take 690 to
+// 740 us, nearly their sum.
 
 #include <type_traits>
 
@@ -353,8 +353,9 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
   uint8_t* const own = lds + wave * 16 * kRow;
   const int64_t k0 = static_cast<int64_t>(block0 + wk) * kBlock8 + lane % 32 * 4;
   const int64_t left_k = x.cols - k0;
-  // Whole lines go past the caches (3% at 19 workers, 16384 x 4096 x 4096); parts of
-  // lines stay for their other parts (11 workers, 500 x 2001 x 1999: 48 us, and 72 past them).
+  // Whole lines go past the caches (19 workers, 2048 x 4096 x 4096: 267 us, and 310 by way of
+  // them; with 16384 tokens 686 and 671); parts of lines stay for their other parts (11
+  // workers, 500 x 2001 x 1999: 68 us, and 72 past them).
   auto store = [&](auto past_caches) {
 #pragma unroll
     for (int k = 0; k < FB; ++k) {
@@ -448,11 +449,11 @@ struct Plan {
 
 // A round of workgroups costs about their time alone on a CU, which for a step of 32
 // tokens is, in units of the largest tile's: 256 x 256, one a CU, 1; two of 128 x 128 on
-// a CU 0.72; three of 64 x 128 0.68 (a round of 512 steps at 16384 x 4096 x 4096 on one card:
-// 574, 411 and 388 us). Few tiles of many tokens leave CUs idle: their tokens are cut
+// a CU 0.72; three of 64 x 128 0.68 (a round of 512 steps on one card: 487 us, 371 and, two
+// thirds full, 320). Few tiles of many tokens leave CUs idle: their tokens are cut
 // into up to 16 shares of at least eight steps, whose sums cost a pass over splits * 4
 // bytes for each value of dw (as long as some 8 steps): one worker's 16384 x 2048 x 4096
-// takes 282 us so, and 464, 383 or 582 us uncut in the three forms.
+// takes 270 us so, and 458, 371 or 572 us uncut in the three forms.
 Plan plan_gradient(int parts, int64_t tokens, int64_t outputs, int64_t inputs, int n) {
   struct Shape {
     int wk, fb, slots;
