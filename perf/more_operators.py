@@ -258,8 +258,8 @@ def _calls(s):
         return gf.linear_backward(s["dy"], s["w"], s["pre"], act, s["residual"])
     if kind == "weight_gradient":
         n, k, g = case["outputs"], case["inputs"], s["grads"]
-        gf.weight_gradient(s["dy"], s["x"], s["counts"], out=g[:, :n * k].view(-1, n, k),
-                           dbias=g[:, n * k:])
+        gf.linear_weight_gradient(s["dy"], s["x"], s["counts"], out=g[:, :n * k].view(-1, n, k),
+                                  dbias=g[:, n * k:])
         return g
     rms, scale = case["rms"], s["scale"]
     if kind == "residual_norm":
