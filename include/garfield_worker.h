@@ -160,6 +160,156 @@ garfield_status garfield_weight_gradient(const void* dy, int type, int64_t token
                                          float* dbias, int64_t ld_dbias, void* workspace,
                                          size_t workspace_bytes, void* stream);
 
+/* What is done with a linear layer's sums. */
+typedef enum garfield_activation {
+  GARFIELD_NO_ACTIVATION = 0,
+  GARFIELD_RELU = 1,      /* max(p, 0); its slope at 0 is 0 */
+  GARFIELD_GELU = 2,      /* p Phi(p), Phi the normal distribution's */
+  GARFIELD_GELU_TANH = 3, /* p (1 + tanh(sqrt(2 / pi) (p + 0.044715 p^3))) / 2 */
+  GARFIELD_SILU = 4       /* p / (1 + exp(-p)) */
+} garfield_activation;
+
+/*
+ * A linear layer of 16- or 32-bit matrices with its epilogue: of every token and output
+ *   p = sum_k x[t][k] w[j][k] + bias[j],  out[t][j] = act(p) + residual[t][j].
+ * x (tokens x inputs), w (outputs x inputs), residual and out (tokens x outputs) are of
+ * `type`; bias (outputs values) is of btype: GARFIELD_F32 or `type`. bias, residual and pre
+ * may be NULL; pre gets p, rounded to `type`, for the backward pass. Sums are fp32, and out
+ * and pre are rounded once. fp32 products are those of fp32 values.
+ * A row of x or w is at most 2^24 columns (GARFIELD_ETOOBIG beyond). The workspace holds
+ * matrices whose rows the product cannot read as they are (their address, distance or length
+ * no multiple of 16 bytes), once more, and the fp32 sums of a few columns' shares.
+ */
+size_t garfield_linear_workspace(const void* x, int type, int64_t tokens, int64_t inputs,
+                                 int64_t ldx, const void* w, int64_t outputs, int64_t ldw);
+garfield_status garfield_linear(const void* x, int type, int64_t tokens, int64_t inputs,
+                                int64_t ldx, const void* w, int64_t outputs, int64_t ldw,
+                                const void* bias, int btype, int activation, const void* residual,
+                                int64_t ld_residual, void* out, int64_t ld_out, void* pre,
+                                int64_t ld_pre, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
+ * The gradient of a linear layer's input, on through what came before it:
+ *   dx[t][k] = act'(pre[t][k]) sum_j dy[t][j] w[j][k] + residual[t][k],
+ * with pre what garfield_linear kept of the layer before (tokens x inputs, NULL with
+ * GARFIELD_NO_ACTIVATION), and residual a gradient that reaches the same place by another way
+ * (NULL: none). All matrices are of `type`; sums are fp32, dx is rounded once.
+ */
+size_t garfield_linear_backward_workspace(const void* dy, int type, int64_t tokens,
+                                          int64_t outputs, int64_t lddy, const void* w,
+                                          int64_t inputs, int64_t ldw);
+garfield_status garfield_linear_backward(const void* dy, int type, int64_t tokens, int64_t outputs,
+                                         int64_t lddy, const void* w, int64_t inputs, int64_t ldw,
+                                         int activation, const void* pre, int64_t ld_pre,
+                                         const void* residual, int64_t ld_residual, void* dx,
+                                         int64_t lddx, void* workspace, size_t workspace_bytes,
+                                         void* stream);
+
+/* dp = act'(pre) dy, values of `type` (rows x cols): from the gradient of garfield_linear's out
+ * to that of its sums. */
+garfield_status garfield_activation_backward(const void* dy, int type, int64_t rows, int64_t cols,
+                                             int64_t lddy, int activation, const void* pre,
+                                             int64_t ld_pre, void* dp, int64_t lddp, void* stream);
+
+/*
+ * garfield_weight_gradient of an input that is no checkpoint: x (tokens x inputs) is of dy's
+ * type. At most 2^24 outputs and inputs.
+ */
+size_t garfield_linear_weight_gradient_workspace(const void* dy, int type, int64_t tokens,
+                                                 int64_t outputs, int64_t lddy, const void* x,
+                                                 int64_t inputs, int64_t ldx, int n,
+                                                 const int64_t* counts);
+garfield_status garfield_linear_weight_gradient(const void* dy, int type, int64_t tokens,
+                                                int64_t outputs, int64_t lddy, const void* x,
+                                                int64_t inputs, int64_t ldx, int n,
+                                                const int64_t* counts, float* dw, int64_t ld_dw,
+                                                float* dbias, int64_t ld_dbias, void* workspace,
+                                                size_t workspace_bytes, void* stream);
+
+/*
+ * The residual around a block, with the norms before and after it: of every token
+ *   s = scale * x + gate * N_post(h),  y = N(s),
+ * where x is the residual stream, h the block's result, and N a norm of rows
+ *   N(v)_c = (v_c - mean) * rstd * weight_c + bias_c  (rms: v_c * rstd * weight_c)
+ * with mean = sum_c v_c / cols and rstd = (sum_c (v_c - mean)^2 / cols + eps)^(-1/2); with rms
+ * the mean is 0 and there are no biases. x, h, s and y (rows x cols) are of `type`; weights,
+ * biases and a gate of columns (cols values each) of wtype: GARFIELD_F32 or `type`.
+ */
+typedef struct garfield_residual_block {
+  int type, wtype;
+  int64_t rows, cols;
+  int rms;
+  float eps, scale;
+  const void *weight, *bias;           /* of N; weight NULL: no norm after, no y */
+  const void *post_weight, *post_bias; /* of N_post; post_weight NULL: N_post(h) = h */
+  const void* gate;                    /* NULL: 1 */
+  int64_t ld_gate; /* 0: gate is one value a column; else a matrix of `type` like h */
+} garfield_residual_block;
+
+/*
+ * s, y and each row's statistics (rows fp32 values; the means are not written with rms and
+ * may be NULL then, those of a norm that is not there too). y and y8 (the checkpoint of y's
+ * values in 32 bits) may be NULL. s is rounded once; y is formed from s in 32 bits, before
+ * it is rounded. The means' sums are kept as garfield_layernorm keeps them.
+ */
+garfield_status garfield_residual_norm(const garfield_residual_block* b, const void* x,
+                                       int64_t ldx, const void* h, int64_t ldh, void* s,
+                                       int64_t lds, void* y, int64_t ldy, float* mean, float* rstd,
+                                       float* post_mean, float* post_rstd,
+                                       const garfield_block8* y8, void* stream);
+
+/* The gradients of each worker: worker w's row at weight + w * ld_weight, and so on (cols
+ * fp32 values each). NULL where one is not asked for, or has no parameter. */
+typedef struct garfield_residual_gradients {
+  float *weight, *bias, *post_weight, *post_bias, *gate;
+  int64_t ld_weight, ld_bias, ld_post_weight, ld_post_bias, ld_gate;
+} garfield_residual_gradients;
+
+/*
+ * Its backward pass, from the gradients of s by other ways (ds) and of y (dy): NULL where
+ * there is none, dy also where b->weight is NULL. With g the whole gradient of s,
+ *   g = ds + N'(dy),  dx = scale * g,  dh = N_post'(gate * g),
+ *   dgate = g * N_post(h)  (by tokens: dgate, a matrix of `type`; by columns: in `gradients`),
+ * and the weights' and biases' gradients as garfield_layernorm_backward's. s (needed where dy
+ * is given), h and the statistics are the forward pass's. dx, dh and dgate may be NULL.
+ */
+size_t garfield_residual_norm_backward_workspace(const garfield_residual_block* b, int n,
+                                                 const int64_t* counts);
+garfield_status garfield_residual_norm_backward(
+    const garfield_residual_block* b, const void* ds, int64_t ldds, const void* dy, int64_t lddy,
+    const void* s, int64_t lds, const void* h, int64_t ldh, const float* mean, const float* rstd,
+    const float* post_mean, const float* post_rstd, void* dx, int64_t lddx, void* dh,
+    int64_t lddh, void* dgate, int64_t lddgate, int n, const int64_t* counts,
+    const garfield_residual_gradients* gradients, void* workspace, size_t workspace_bytes,
+    void* stream);
+
+/* A tensor of every worker's gradient: worker w's `length` values of `type`, next to each
+ * other, at values + w * ld elements. */
+typedef struct garfield_gradient {
+  void* values;
+  int64_t length, ld;
+  int type;
+} garfield_gradient;
+
+/*
+ * Each worker's gradient norm over `count` tensors (a HOST array, read before the call
+ * returns), norms[w] = (sum of all its values' squares)^(1/2), and its gradient clipped:
+ *   out = value * (norm > max_norm ? max_norm / norm : 1),
+ * the tensors one after the other into worker w's row of fp32 values at out + w * ld_out, or
+ * in place with out NULL (values are then rounded once to their type, and tensors must not
+ * share memory: GARFIELD_EINVAL). Squares are added up in 64 bits. A worker with an infinite
+ * value gets zeros and, for the infinities, NaN; one with a NaN gets NaN throughout: norms says
+ * which. At most 2^20 tensors, each of at most 2^34 values a worker (GARFIELD_ETOOBIG).
+ */
+size_t garfield_clip_workspace(const garfield_gradient* tensors, int count, int n);
+garfield_status garfield_gradient_norms(const garfield_gradient* tensors, int count, int n,
+                                        float* norms, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+garfield_status garfield_clip_gradients(const garfield_gradient* tensors, int count, int n,
+                                        float max_norm, float* norms, float* out, int64_t ld_out,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

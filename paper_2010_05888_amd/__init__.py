@@ -639,5 +639,7 @@ def distance_engine(n: int, d: int) -> str:
     return {0: "none", 1: "direct", 2: "gram"}[load().garfield_tuning_distance_engine(n, d)]
 
 
-from .worker import (Checkpoint, LayerNorm, checkpoint, layernorm,  # noqa: E402
-                     layernorm_backward, linear8, weight_gradient)
+from .worker import (Checkpoint, LayerNorm, Linear, ResidualNorm, ResidualNormBackward,  # noqa: E402
+                     activation_backward, checkpoint, clip_gradients, gradient_norms, layernorm,
+                     layernorm_backward, linear, linear8, linear_backward, linear_weight_gradient,
+                     residual_norm, residual_norm_backward, weight_gradient)

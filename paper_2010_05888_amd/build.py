@@ -21,7 +21,8 @@ LIB = os.path.join(HERE, "libgarfield.so")
 
 SOURCES = ["dist.hip", "ring_direct.hip", "select.hip", "aggregate.hip", "byzantine.hip", "segtable.hip",
            "contract.hip", "garfield_api.cpp", "timing.cpp",
-           "layernorm.hip", "block8.hip", "linear8.hip", "weight_gradient.hip", "worker_api.cpp"]
+           "layernorm.hip", "block8.hip", "linear8.hip", "weight_gradient.hip", "linear.hip",
+           "residual_norm.hip", "clip.hip", "worker_api.cpp"]
 
 ARCH = "gfx950"
 FLAGS = [

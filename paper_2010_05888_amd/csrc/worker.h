@@ -79,4 +79,83 @@ size_t weight_gradient_bytes(int type, int64_t tokens, int64_t outputs, int64_t 
                              const void* dy, int64_t lddy, int n, const int64_t* counts);
 hipError_t enqueue_weight_gradient(const WeightGradient& a, void* workspace, hipStream_t s);
 
+// out = act(A B^T + bias) + residual, or slope(before) * (A B^T) + residual. A and B are rows
+// of the sum's columns or, where `across`, have the sum's columns as rows.
+struct Epilogue {
+  const void* bias = nullptr;
+  bool bias_f32 = true;
+  int activation = GARFIELD_NO_ACTIVATION;
+  const void* before = nullptr;  // what the slope is taken at; null: a forward pass
+  int64_t ld_before = 0;
+  const void* residual = nullptr;
+  int64_t ld_residual = 0;
+  void* out = nullptr;
+  int64_t ld_out = 0;
+  void* pre = nullptr;
+  int64_t ld_pre = 0;
+};
+struct Operand {
+  const void* p = nullptr;
+  int64_t ld = 0;
+  bool across = false;
+};
+struct Product {
+  int type = GARFIELD_F32;
+  int64_t rows = 0, cols = 0, depth = 0;
+  Operand a, b;
+  Epilogue to;
+};
+size_t product_bytes(const Product& p);
+hipError_t enqueue_product(const Product& p, void* workspace, hipStream_t s);
+
+hipError_t enqueue_activation_backward(const void* dy, int64_t lddy, const void* pre,
+                                       int64_t ld_pre, int activation, void* dp, int64_t lddp,
+                                       int type, int64_t rows, int64_t cols, hipStream_t s);
+
+struct DenseGradient {
+  const void *dy, *x;
+  int type;
+  int64_t tokens, outputs, inputs, lddy, ldx;
+  int n;
+  const int64_t* counts;
+  float* dw;
+  int64_t ld_dw;
+  float* dbias;
+  int64_t ld_dbias;
+};
+size_t dense_gradient_bytes(const DenseGradient& a);
+hipError_t enqueue_dense_gradient(const DenseGradient& a, void* workspace, hipStream_t s);
+
+struct ResidualNorm {
+  garfield_residual_block b;
+  const void *x, *h;
+  int64_t ldx, ldh;
+  double share;  // 1 / cols
+  void *s, *y;
+  int64_t lds, ldy;
+  float *mean, *rstd, *post_mean, *post_rstd;
+  garfield_block8 y8;  // values null: not asked for
+};
+hipError_t enqueue_residual_norm(const ResidualNorm& a, hipStream_t s);
+
+struct ResidualNormBackward {
+  garfield_residual_block b;
+  const void *ds, *dy, *s, *h;
+  int64_t ldds, lddy, lds, ldh;
+  const float *mean, *rstd, *post_mean, *post_rstd;
+  void *dx, *dh, *dgate;
+  int64_t lddx, lddh, lddgate;
+  garfield_residual_gradients to;
+};
+Chunks residual_norm_backward_chunks(const garfield_residual_block& b, int n,
+                                     const int64_t* counts);
+size_t residual_norm_backward_bytes(const garfield_residual_block& b, const Chunks& c);
+hipError_t enqueue_residual_norm_backward(const ResidualNormBackward& a, const Chunks& c,
+                                          void* workspace, hipStream_t s);
+
+// max_norm NaN: norms alone. out null: in place.
+size_t clip_bytes(const garfield_gradient* tensors, int count, int n);
+hipError_t enqueue_clip(const garfield_gradient* tensors, int count, int n, float max_norm,
+                        float* norms, float* out, int64_t ld_out, void* workspace, hipStream_t s);
+
 }  // namespace garfield

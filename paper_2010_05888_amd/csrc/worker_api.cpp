@@ -3,6 +3,11 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
 #include "garfield_worker.h"
 #include "internal.h"
 #include "worker.h"
@@ -18,6 +23,9 @@ constexpr int64_t kMaxBlocks = int64_t{1} << 27;  // of one matrix, padded
 // Weight gradients address 32 tokens with 32 bits.
 constexpr int64_t kMaxOutputs = int64_t{1} << 24;
 constexpr int64_t kMaxStride = int64_t{1} << 26;
+constexpr int64_t kMaxDepth = int64_t{1} << 24;  // a dense product's columns that are added up
+constexpr int kMaxTensors = 1 << 20;
+constexpr int64_t kMaxLength = int64_t{1} << 34;
 
 garfield_status status_of(hipError_t e) {
   if (e == hipSuccess) return GARFIELD_OK;
@@ -74,6 +82,135 @@ bool gradient_ok(const float* p, int n, int64_t length, int64_t ld) {
 
 bool workspace_ok(const void* p, size_t bytes, size_t need) {
   return need == 0 || (p && aligned(p, 256) && bytes >= need);
+}
+
+bool is_activation(int a) { return a >= GARFIELD_NO_ACTIVATION && a <= GARFIELD_SILU; }
+
+garfield_status check_product(int64_t rows, int64_t cols, int64_t depth) {
+  garfield_status st = check_size(rows, depth);
+  if (st == GARFIELD_OK) st = check_size(cols, depth);
+  if (st == GARFIELD_OK) st = check_size(rows, cols);
+  return st == GARFIELD_OK && depth > kMaxDepth ? GARFIELD_ETOOBIG : st;
+}
+
+Product forward_product(const void* x, int type, int64_t tokens, int64_t inputs, int64_t ldx,
+                        const void* w, int64_t outputs, int64_t ldw) {
+  Product p;
+  p.type = type;
+  p.rows = tokens;
+  p.cols = outputs;
+  p.depth = inputs;
+  p.a = {x, ldx, false};
+  p.b = {w, ldw, false};
+  return p;
+}
+
+Product backward_product(const void* dy, int type, int64_t tokens, int64_t outputs, int64_t lddy,
+                         const void* w, int64_t inputs, int64_t ldw) {
+  Product p;
+  p.type = type;
+  p.rows = tokens;
+  p.cols = inputs;
+  p.depth = outputs;
+  p.a = {dy, lddy, false};
+  p.b = {w, ldw, true};
+  return p;
+}
+
+DenseGradient dense_gradient(const void* dy, int type, int64_t tokens, int64_t outputs,
+                             int64_t lddy, const void* x, int64_t inputs, int64_t ldx, int n,
+                             const int64_t* counts) {
+  DenseGradient a = {};
+  a.dy = dy;
+  a.x = x;
+  a.type = type;
+  a.tokens = tokens;
+  a.outputs = outputs;
+  a.inputs = inputs;
+  a.lddy = lddy;
+  a.ldx = ldx;
+  a.n = n;
+  a.counts = counts;
+  return a;
+}
+
+garfield_status check_dense_gradient(int type, int64_t tokens, int64_t outputs, int64_t inputs,
+                                     int n, const int64_t* counts) {
+  if (!is_type(type)) return GARFIELD_EINVAL;
+  garfield_status st = check_size(tokens, outputs);
+  if (st == GARFIELD_OK) st = check_size(tokens, inputs);
+  if (st == GARFIELD_OK) st = check_size(outputs, inputs);
+  if (st == GARFIELD_OK) st = check_counts(n, counts, tokens);
+  if (st == GARFIELD_OK && (outputs > kMaxOutputs || inputs > kMaxOutputs)) return GARFIELD_ETOOBIG;
+  return st;
+}
+
+garfield_status check_block(const garfield_residual_block* b) {
+  if (!b || !is_type(b->type) || (b->wtype != GARFIELD_F32 && b->wtype != b->type))
+    return GARFIELD_EINVAL;
+  const garfield_status st = check_size(b->rows, b->cols);
+  if (st != GARFIELD_OK) return st;
+  const int64_t bytes = element_bytes(b->wtype);
+  auto parameter = [&](const void* p) { return !p || vector_ok(p, bytes, b->cols); };
+  if (b->cols == 0 || !(b->eps >= 0.0f) || !parameter(b->weight) || !parameter(b->bias) ||
+      !parameter(b->post_weight) || !parameter(b->post_bias) || (b->bias && !b->weight) ||
+      (b->post_bias && !b->post_weight) || (b->rms && (b->bias || b->post_bias)))
+    return GARFIELD_EINVAL;
+  if (b->gate && (b->ld_gate == 0 ? !parameter(b->gate)
+                                  : !matrix_ok(b->gate, b->type, b->rows, b->cols, b->ld_gate)))
+    return GARFIELD_EINVAL;
+  return GARFIELD_OK;
+}
+
+garfield_status check_tensors(const garfield_gradient* t, int count, int n) {
+  if (count < 0 || n < 1 || (count > 0 && !t)) return GARFIELD_EINVAL;
+  if (n > GARFIELD_NMAX || count > kMaxTensors) return GARFIELD_ETOOBIG;
+  for (int i = 0; i < count; ++i) {
+    if (!is_type(t[i].type) || t[i].length < 0) return GARFIELD_EINVAL;
+    if (t[i].length > kMaxLength) return GARFIELD_ETOOBIG;
+  }
+  return GARFIELD_OK;
+}
+
+bool tensors_ok(const garfield_gradient* t, int count, int n) {
+  for (int i = 0; i < count; ++i)
+    if (t[i].length > 0 && (!t[i].values || !aligned(t[i].values, element_bytes(t[i].type)) ||
+                            (n > 1 && t[i].ld < t[i].length)))
+      return false;
+  return true;
+}
+
+// Whether no two of the tensors have a byte in common. Tensors whose ranges overlap may still
+// be columns of one matrix: rows equally far apart, and no columns shared.
+bool tensors_apart(const garfield_gradient* t, int count, int n) {
+  struct Range {
+    uintptr_t first, end;
+    uintptr_t apart, length;  // bytes
+  };
+  std::vector<Range> all;
+  all.reserve(count);
+  for (int i = 0; i < count; ++i) {
+    if (t[i].length == 0) continue;
+    const uintptr_t b = element_bytes(t[i].type), p = reinterpret_cast<uintptr_t>(t[i].values);
+    const uintptr_t apart = n > 1 ? t[i].ld * b : 0, length = t[i].length * b;
+    all.push_back({p, p + apart * (n - 1) + length, apart, length});
+  }
+  std::sort(all.begin(), all.end(), [](const Range& x, const Range& y) { return x.first < y.first; });
+  // In a group of ranges that overlap, all must be columns of the first one's matrix: its
+  // rows, in which no column starts before the last one's end, and which wrap round once.
+  for (size_t i = 0; i < all.size();) {
+    const Range& r = all[i];
+    uintptr_t end = r.end, used = r.length;
+    size_t k = i + 1;
+    for (; k < all.size() && all[k].first < end; ++k) {
+      const uintptr_t at = all[k].first - r.first;
+      if (n == 1 || all[k].apart != r.apart || at < used || at + all[k].length > r.apart) return false;
+      used = at + all[k].length;
+      end = std::max(end, all[k].end);
+    }
+    i = k;
+  }
+  return true;
 }
 
 }  // namespace
@@ -265,6 +402,265 @@ garfield_status garfield_weight_gradient(const void* dy, int type, int64_t token
   a.dbias = dbias;
   a.ld_dbias = ld_dbias;
   return status_of(enqueue_weight_gradient(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t garfield_linear_workspace(const void* x, int type, int64_t tokens, int64_t inputs,
+                                 int64_t ldx, const void* w, int64_t outputs, int64_t ldw) {
+  if (!is_type(type) || check_product(tokens, outputs, inputs) != GARFIELD_OK) return 0;
+  return product_bytes(forward_product(x, type, tokens, inputs, ldx, w, outputs, ldw));
+}
+
+garfield_status garfield_linear(const void* x, int type, int64_t tokens, int64_t inputs,
+                                int64_t ldx, const void* w, int64_t outputs, int64_t ldw,
+                                const void* bias, int btype, int activation, const void* residual,
+                                int64_t ld_residual, void* out, int64_t ld_out, void* pre,
+                                int64_t ld_pre, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  if (!is_type(type) || (bias && btype != GARFIELD_F32 && btype != type) ||
+      !is_activation(activation))
+    return GARFIELD_EINVAL;
+  const garfield_status st = check_product(tokens, outputs, inputs);
+  if (st != GARFIELD_OK) return st;
+  if (!matrix_ok(x, type, tokens, inputs, ldx) || !matrix_ok(w, type, outputs, inputs, ldw) ||
+      (bias && !vector_ok(bias, element_bytes(btype), outputs)) ||
+      (residual && !matrix_ok(residual, type, tokens, outputs, ld_residual)) ||
+      !matrix_ok(out, type, tokens, outputs, ld_out) ||
+      (pre && !matrix_ok(pre, type, tokens, outputs, ld_pre)))
+    return GARFIELD_EINVAL;
+  Product p = forward_product(x, type, tokens, inputs, ldx, w, outputs, ldw);
+  if (!workspace_ok(workspace, workspace_bytes, product_bytes(p))) return GARFIELD_EINVAL;
+  if (tokens == 0 || outputs == 0) return GARFIELD_OK;
+  p.to.bias = bias;
+  p.to.bias_f32 = btype == GARFIELD_F32;
+  p.to.activation = activation;
+  p.to.residual = residual;
+  p.to.ld_residual = ld_residual;
+  p.to.out = out;
+  p.to.ld_out = ld_out;
+  p.to.pre = pre;
+  p.to.ld_pre = ld_pre;
+  return status_of(enqueue_product(p, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t garfield_linear_backward_workspace(const void* dy, int type, int64_t tokens,
+                                          int64_t outputs, int64_t lddy, const void* w,
+                                          int64_t inputs, int64_t ldw) {
+  if (!is_type(type) || check_product(tokens, inputs, outputs) != GARFIELD_OK) return 0;
+  return product_bytes(backward_product(dy, type, tokens, outputs, lddy, w, inputs, ldw));
+}
+
+garfield_status garfield_linear_backward(const void* dy, int type, int64_t tokens, int64_t outputs,
+                                         int64_t lddy, const void* w, int64_t inputs, int64_t ldw,
+                                         int activation, const void* pre, int64_t ld_pre,
+                                         const void* residual, int64_t ld_residual, void* dx,
+                                         int64_t lddx, void* workspace, size_t workspace_bytes,
+                                         void* stream) {
+  if (!is_type(type) || !is_activation(activation)) return GARFIELD_EINVAL;
+  const garfield_status st = check_product(tokens, inputs, outputs);
+  if (st != GARFIELD_OK) return st;
+  if (!matrix_ok(dy, type, tokens, outputs, lddy) || !matrix_ok(w, type, outputs, inputs, ldw) ||
+      (activation != GARFIELD_NO_ACTIVATION && !matrix_ok(pre, type, tokens, inputs, ld_pre)) ||
+      (residual && !matrix_ok(residual, type, tokens, inputs, ld_residual)) ||
+      !matrix_ok(dx, type, tokens, inputs, lddx))
+    return GARFIELD_EINVAL;
+  Product p = backward_product(dy, type, tokens, outputs, lddy, w, inputs, ldw);
+  if (!workspace_ok(workspace, workspace_bytes, product_bytes(p))) return GARFIELD_EINVAL;
+  if (tokens == 0 || inputs == 0) return GARFIELD_OK;
+  p.to.activation = activation;
+  p.to.before = activation != GARFIELD_NO_ACTIVATION ? pre : nullptr;
+  p.to.ld_before = ld_pre;
+  p.to.residual = residual;
+  p.to.ld_residual = ld_residual;
+  p.to.out = dx;
+  p.to.ld_out = lddx;
+  return status_of(enqueue_product(p, workspace, static_cast<hipStream_t>(stream)));
+}
+
+garfield_status garfield_activation_backward(const void* dy, int type, int64_t rows, int64_t cols,
+                                             int64_t lddy, int activation, const void* pre,
+                                             int64_t ld_pre, void* dp, int64_t lddp,
+                                             void* stream) {
+  if (!is_type(type) || !is_activation(activation)) return GARFIELD_EINVAL;
+  const garfield_status st = check_size(rows, cols);
+  if (st != GARFIELD_OK) return st;
+  if (!matrix_ok(dy, type, rows, cols, lddy) || !matrix_ok(pre, type, rows, cols, ld_pre) ||
+      !matrix_ok(dp, type, rows, cols, lddp))
+    return GARFIELD_EINVAL;
+  if (rows == 0 || cols == 0) return GARFIELD_OK;
+  return status_of(enqueue_activation_backward(dy, lddy, pre, ld_pre, activation, dp, lddp, type,
+                                               rows, cols, static_cast<hipStream_t>(stream)));
+}
+
+size_t garfield_linear_weight_gradient_workspace(const void* dy, int type, int64_t tokens,
+                                                 int64_t outputs, int64_t lddy, const void* x,
+                                                 int64_t inputs, int64_t ldx, int n,
+                                                 const int64_t* counts) {
+  if (check_dense_gradient(type, tokens, outputs, inputs, n, counts) != GARFIELD_OK) return 0;
+  return dense_gradient_bytes(
+      dense_gradient(dy, type, tokens, outputs, lddy, x, inputs, ldx, n, counts));
+}
+
+garfield_status garfield_linear_weight_gradient(const void* dy, int type, int64_t tokens,
+                                                int64_t outputs, int64_t lddy, const void* x,
+                                                int64_t inputs, int64_t ldx, int n,
+                                                const int64_t* counts, float* dw, int64_t ld_dw,
+                                                float* dbias, int64_t ld_dbias, void* workspace,
+                                                size_t workspace_bytes, void* stream) {
+  const garfield_status st = check_dense_gradient(type, tokens, outputs, inputs, n, counts);
+  if (st != GARFIELD_OK) return st;
+  const int64_t length = outputs * inputs;
+  if (!matrix_ok(dy, type, tokens, outputs, lddy) || !matrix_ok(x, type, tokens, inputs, ldx) ||
+      (length > 0 && !dw) || !gradient_ok(dw, n, length, ld_dw) ||
+      !gradient_ok(dbias, n, outputs, ld_dbias))
+    return GARFIELD_EINVAL;
+  DenseGradient a = dense_gradient(dy, type, tokens, outputs, lddy, x, inputs, ldx, n, counts);
+  if (!workspace_ok(workspace, workspace_bytes, dense_gradient_bytes(a))) return GARFIELD_EINVAL;
+  if (outputs == 0) return GARFIELD_OK;
+  a.dw = dw;
+  a.ld_dw = ld_dw;
+  a.dbias = dbias;
+  a.ld_dbias = ld_dbias;
+  return status_of(enqueue_dense_gradient(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+garfield_status garfield_residual_norm(const garfield_residual_block* b, const void* x,
+                                       int64_t ldx, const void* h, int64_t ldh, void* s,
+                                       int64_t lds, void* y, int64_t ldy, float* mean, float* rstd,
+                                       float* post_mean, float* post_rstd,
+                                       const garfield_block8* y8, void* stream) {
+  const garfield_status st = check_block(b);
+  if (st != GARFIELD_OK) return st;
+  const int64_t rows = b->rows, cols = b->cols;
+  auto stats_ok = [&](const void* norm, float* m, float* r) {
+    return !norm || (vector_ok(r, 4, rows) && (b->rms || vector_ok(m, 4, rows)));
+  };
+  if (!matrix_ok(x, b->type, rows, cols, ldx) || !matrix_ok(h, b->type, rows, cols, ldh) ||
+      !matrix_ok(s, b->type, rows, cols, lds) || (y && !matrix_ok(y, b->type, rows, cols, ldy)) ||
+      (!b->weight && (y || y8)) || !stats_ok(b->weight, mean, rstd) ||
+      !stats_ok(b->post_weight, post_mean, post_rstd) || (y8 && !block8_ok(y8, rows, cols)))
+    return GARFIELD_EINVAL;
+  if (rows == 0) return GARFIELD_OK;
+  ResidualNorm a = {};
+  a.b = *b;
+  a.x = x;
+  a.h = h;
+  a.ldx = ldx;
+  a.ldh = ldh;
+  a.share = 1.0 / static_cast<double>(cols);
+  a.s = s;
+  a.y = y;
+  a.lds = lds;
+  a.ldy = ldy;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.post_mean = post_mean;
+  a.post_rstd = post_rstd;
+  if (y8) a.y8 = *y8;
+  return status_of(enqueue_residual_norm(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t garfield_residual_norm_backward_workspace(const garfield_residual_block* b, int n,
+                                                 const int64_t* counts) {
+  if (check_block(b) != GARFIELD_OK || check_counts(n, counts, b->rows) != GARFIELD_OK) return 0;
+  return residual_norm_backward_bytes(*b, residual_norm_backward_chunks(*b, n, counts));
+}
+
+garfield_status garfield_residual_norm_backward(
+    const garfield_residual_block* b, const void* ds, int64_t ldds, const void* dy, int64_t lddy,
+    const void* s, int64_t lds, const void* h, int64_t ldh, const float* mean, const float* rstd,
+    const float* post_mean, const float* post_rstd, void* dx, int64_t lddx, void* dh,
+    int64_t lddh, void* dgate, int64_t lddgate, int n, const int64_t* counts,
+    const garfield_residual_gradients* gradients, void* workspace, size_t workspace_bytes,
+    void* stream) {
+  garfield_status st = check_block(b);
+  if (st == GARFIELD_OK) st = check_counts(n, counts, b->rows);
+  if (st != GARFIELD_OK) return st;
+  const int64_t rows = b->rows, cols = b->cols;
+  auto given = [&](const void* p, int64_t ld) { return matrix_ok(p, b->type, rows, cols, ld); };
+  auto stats_ok = [&](const float* m, const float* r) {
+    return vector_ok(r, 4, rows) && (b->rms || vector_ok(m, 4, rows));
+  };
+  const garfield_residual_gradients to = gradients ? *gradients : garfield_residual_gradients{};
+  const bool by_tokens = b->gate && b->ld_gate != 0;
+  if ((!ds && !dy && rows > 0) || (ds && !given(ds, ldds)) ||
+      (dy && (!b->weight || !given(dy, lddy) || !given(s, lds) || !stats_ok(mean, rstd))) ||
+      !given(h, ldh) || (b->post_weight && !stats_ok(post_mean, post_rstd)) ||
+      (dx && !given(dx, lddx)) || (dh && !given(dh, lddh)) ||
+      (dgate && (!by_tokens || !given(dgate, lddgate))) ||
+      (to.weight && !b->weight) || (to.bias && (!b->weight || b->rms)) ||
+      (to.post_weight && !b->post_weight) || (to.post_bias && (!b->post_weight || b->rms)) ||
+      (to.gate && (!b->gate || by_tokens)) || !gradient_ok(to.weight, n, cols, to.ld_weight) ||
+      !gradient_ok(to.bias, n, cols, to.ld_bias) ||
+      !gradient_ok(to.post_weight, n, cols, to.ld_post_weight) ||
+      !gradient_ok(to.post_bias, n, cols, to.ld_post_bias) ||
+      !gradient_ok(to.gate, n, cols, to.ld_gate))
+    return GARFIELD_EINVAL;
+  const Chunks chunks = residual_norm_backward_chunks(*b, n, counts);
+  if (!workspace_ok(workspace, workspace_bytes, residual_norm_backward_bytes(*b, chunks)))
+    return GARFIELD_EINVAL;
+  ResidualNormBackward a = {};
+  a.b = *b;
+  a.ds = ds;
+  a.dy = dy;
+  a.s = s;
+  a.h = h;
+  a.ldds = ldds;
+  a.lddy = lddy;
+  a.lds = lds;
+  a.ldh = ldh;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.post_mean = post_mean;
+  a.post_rstd = post_rstd;
+  a.dx = dx;
+  a.dh = dh;
+  a.dgate = dgate;
+  a.lddx = lddx;
+  a.lddh = lddh;
+  a.lddgate = lddgate;
+  a.to = to;
+  return status_of(
+      enqueue_residual_norm_backward(a, chunks, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t garfield_clip_workspace(const garfield_gradient* tensors, int count, int n) {
+  if (check_tensors(tensors, count, n) != GARFIELD_OK) return 0;
+  return clip_bytes(tensors, count, n);
+}
+
+garfield_status garfield_gradient_norms(const garfield_gradient* tensors, int count, int n,
+                                        float* norms, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+  const garfield_status st = check_tensors(tensors, count, n);
+  if (st != GARFIELD_OK) return st;
+  if (!tensors_ok(tensors, count, n) || !vector_ok(norms, 4, n) ||
+      !workspace_ok(workspace, workspace_bytes, clip_bytes(tensors, count, n)))
+    return GARFIELD_EINVAL;
+  return status_of(enqueue_clip(tensors, count, n, NAN, norms, nullptr, 0, workspace,
+                                static_cast<hipStream_t>(stream)));
+}
+
+garfield_status garfield_clip_gradients(const garfield_gradient* tensors, int count, int n,
+                                        float max_norm, float* norms, float* out, int64_t ld_out,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  const garfield_status st = check_tensors(tensors, count, n);
+  if (st != GARFIELD_OK) return st;
+  if (!(max_norm >= 0.0f)) return GARFIELD_EINVAL;
+  int64_t d = 0;
+  for (int i = 0; i < count; ++i) d += tensors[i].length;
+  if (d > kMaxLength) return GARFIELD_ETOOBIG;
+  if (!tensors_ok(tensors, count, n) || !vector_ok(norms, 4, n) || !gradient_ok(out, n, d, ld_out) ||
+      !workspace_ok(workspace, workspace_bytes, clip_bytes(tensors, count, n)))
+    return GARFIELD_EINVAL;
+  if (!out) {
+    try {
+      if (!tensors_apart(tensors, count, n)) return GARFIELD_EINVAL;
+    } catch (const std::bad_alloc&) {
+      return GARFIELD_ENOMEM;
+    }
+  }
+  return status_of(enqueue_clip(tensors, count, n, max_norm, norms, out, ld_out, workspace,
+                                static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

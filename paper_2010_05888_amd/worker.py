@@ -39,9 +39,30 @@ class _Block8(_c.Structure):
                 ("cols", _c.c_int64), ("ld_values", _c.c_int64), ("ld_exponents", _c.c_int64)]
 
 
+class _ResidualBlock(_c.Structure):
+    _fields_ = [("type", _c.c_int), ("wtype", _c.c_int), ("rows", _c.c_int64),
+                ("cols", _c.c_int64), ("rms", _c.c_int), ("eps", _c.c_float),
+                ("scale", _c.c_float), ("weight", _c.c_void_p), ("bias", _c.c_void_p),
+                ("post_weight", _c.c_void_p), ("post_bias", _c.c_void_p), ("gate", _c.c_void_p),
+                ("ld_gate", _c.c_int64)]
+
+
+class _ResidualGradients(_c.Structure):
+    _fields_ = [(name, _c.c_void_p) for name in ("weight", "bias", "post_weight", "post_bias",
+                                                 "gate")] + \
+               [("ld_" + name, _c.c_int64) for name in ("weight", "bias", "post_weight",
+                                                        "post_bias", "gate")]
+
+
+class _Gradient(_c.Structure):
+    _fields_ = [("values", _c.c_void_p), ("length", _c.c_int64), ("ld", _c.c_int64),
+                ("type", _c.c_int)]
+
+
 _vp, _i32, _i64, _sz, _f32 = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_size_t, _c.c_float
 _b8 = _c.POINTER(_Block8)
 _counts_p = _c.POINTER(_i64)
+_rb, _gradients_p = _c.POINTER(_ResidualBlock), _c.POINTER(_Gradient)
 _SIGNATURES = {
     "garfield_checkpoint": (_i32, [_vp, _i32, _i64, _i64, _i64, _i32, _b8, _vp]),
     "garfield_restore": (_i32, [_b8, _vp, _i32, _i64, _vp]),
@@ -57,6 +78,29 @@ _SIGNATURES = {
                                                  _counts_p]),
     "garfield_weight_gradient": (_i32, [_vp, _i32, _i64, _i64, _i64, _b8, _i32, _counts_p, _vp,
                                         _i64, _vp, _i64, _vp, _sz, _vp]),
+    "garfield_linear_workspace": (_sz, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _i64]),
+    "garfield_linear": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i32, _i32, _vp,
+                               _i64, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "garfield_linear_backward_workspace": (_sz, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _i64]),
+    "garfield_linear_backward": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _i32, _vp,
+                                        _i64, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "garfield_activation_backward": (_i32, [_vp, _i32, _i64, _i64, _i64, _i32, _vp, _i64, _vp,
+                                            _i64, _vp]),
+    "garfield_linear_weight_gradient_workspace": (_sz, [_vp, _i32, _i64, _i64, _i64, _vp, _i64,
+                                                        _i64, _i32, _counts_p]),
+    "garfield_linear_weight_gradient": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _i32,
+                                               _counts_p, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "garfield_residual_norm": (_i32, [_rb, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp,
+                                      _vp, _vp, _b8, _vp]),
+    "garfield_residual_norm_backward_workspace": (_sz, [_rb, _i32, _counts_p]),
+    "garfield_residual_norm_backward": (_i32, [_rb, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                                               _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64,
+                                               _i32, _counts_p, _c.POINTER(_ResidualGradients),
+                                               _vp, _sz, _vp]),
+    "garfield_clip_workspace": (_sz, [_gradients_p, _i32, _i32]),
+    "garfield_gradient_norms": (_i32, [_gradients_p, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "garfield_clip_gradients": (_i32, [_gradients_p, _i32, _i32, _f32, _vp, _vp, _i64, _vp, _sz,
+                                       _vp]),
 }
 _fn = {}
 
@@ -352,3 +396,323 @@ def weight_gradient(dy: torch.Tensor, x8: Checkpoint, counts=None,
     _run("garfield_weight_gradient", dev, py, kind, tokens, outputs, ld, x8._at, n, counts,
          out.data_ptr(), ldw, pb, ldb, ws.data_ptr() if need else None, need)
     return out, dbias
+
+
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _activation(name) -> int:
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {list(ACTIVATIONS)}, not {name!r}")
+    return ACTIVATIONS[name]
+
+
+def _like(v, name: str, rows: int, cols: int, x: torch.Tensor):
+    """The pointer and row distance of a matrix of x's type and device (None: none)."""
+    if v is None:
+        return None, 0
+    r, c, ld, _ = _matrix(v, name, x.dtype)
+    if (r, c) != (rows, cols) or v.device != x.device:
+        raise ValueError(f"{name} must be {rows} x {cols} on {x.device}")
+    return v.data_ptr(), ld
+
+
+class Linear(NamedTuple):
+    """What linear() gives: its result, and its sums with the bias (or None)."""
+    out: torch.Tensor
+    pre: torch.Tensor | None
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
+           activation: str | None = None, residual: torch.Tensor | None = None,
+           pre: bool = False) -> Linear:
+    """act(x w^T + bias) + residual (rows of x by rows of w) in x's type, and with pre also
+    x w^T + bias, for the backward pass. activation: None, "relu", "gelu", "gelu_tanh" or
+    "silu"; w and residual are of x's type, bias float32 or of x's. Sums are fp32."""
+    tokens, inputs, ldx, kind = _matrix(x, "x")
+    outputs, k, ldw, _ = _matrix(w, "w", x.dtype)
+    dev, dtype = x.device, x.dtype
+    if k != inputs or w.device != dev:
+        raise ValueError("x and w must have the same columns and device")
+    act = _activation(activation)
+    pb = None if bias is None else _vector(bias, "bias", outputs, _WEIGHTS[dtype], dev)
+    pr, ldr = _like(residual, "residual", tokens, outputs, x)
+    out = _empty((tokens, outputs), dtype=dtype, device=dev)
+    kept = torch.empty_like(out) if pre else None
+    px, pw, ld = x.data_ptr(), w.data_ptr(), outputs or 1
+    ws, need = _workspace("garfield_linear_workspace", dev, px, kind, tokens, inputs, ldx, pw,
+                          outputs, ldw)
+    _run("garfield_linear", dev, px, kind, tokens, inputs, ldx, pw, outputs, ldw, pb,
+         0 if bias is None else TYPES[bias.dtype], act, pr, ldr, out.data_ptr(), ld,
+         kept.data_ptr() if pre else None, ld, ws.data_ptr() if need else None, need)
+    return Linear(out, kept)
+
+
+def linear_backward(dy: torch.Tensor, w: torch.Tensor, pre: torch.Tensor | None = None,
+                    activation: str | None = None,
+                    residual: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of a linear layer's input, dy w, on through what came before it: times
+    the slope at pre of that layer's activation, plus a gradient that comes by another way.
+    All in dy's type; pre is what linear() kept of the layer before."""
+    tokens, outputs, ld, kind = _matrix(dy, "dy")
+    k, inputs, ldw, _ = _matrix(w, "w", dy.dtype)
+    dev = dy.device
+    if k != outputs or w.device != dev:
+        raise ValueError("dy's columns must be w's rows, on one device")
+    act = _activation(activation)
+    if (pre is None) != (activation is None):
+        raise ValueError("pre and activation go together")
+    pp, ldp = _like(pre, "pre", tokens, inputs, dy)
+    pr, ldr = _like(residual, "residual", tokens, inputs, dy)
+    dx = _empty((tokens, inputs), dtype=dy.dtype, device=dev)
+    py, pw = dy.data_ptr(), w.data_ptr()
+    ws, need = _workspace("garfield_linear_backward_workspace", dev, py, kind, tokens, outputs, ld,
+                          pw, inputs, ldw)
+    _run("garfield_linear_backward", dev, py, kind, tokens, outputs, ld, pw, inputs, ldw, act, pp,
+         ldp, pr, ldr, dx.data_ptr(), inputs or 1, ws.data_ptr() if need else None, need)
+    return dx
+
+
+def activation_backward(dy: torch.Tensor, pre: torch.Tensor, activation: str) -> torch.Tensor:
+    """dy times the activation's slope at pre: the gradient of linear()'s sums from that of
+    its result, in dy's type."""
+    rows, cols, ld, kind = _matrix(dy, "dy")
+    if activation is None:
+        raise ValueError("activation_backward needs an activation")
+    act = _activation(activation)
+    if pre is None:
+        raise ValueError("activation_backward needs pre")
+    pp, ldp = _like(pre, "pre", rows, cols, dy)
+    dp = _empty((rows, cols), dtype=dy.dtype, device=dy.device)
+    _run("garfield_activation_backward", dy.device, dy.data_ptr(), kind, rows, cols, ld, act, pp,
+         ldp, dp.data_ptr(), cols or 1)
+    return dp
+
+
+def linear_weight_gradient(dy: torch.Tensor, x: torch.Tensor, counts=None,
+                           out: torch.Tensor | None = None, dbias: torch.Tensor | None = None):
+    """weight_gradient() with the layer's input as it is: x is a matrix of dy's type."""
+    tokens, outputs, ld, kind = _matrix(dy, "dy")
+    rows, inputs, ldx, _ = _matrix(x, "x", dy.dtype)
+    dev = dy.device
+    if rows != tokens or x.device != dev:
+        raise ValueError("x must have dy's rows and device")
+    n, counts = _counted(counts, tokens)
+    out, ldw = _rows_of_workers(out, "out", (n, outputs, inputs), dev)
+    pb, ldb = None, 0
+    if dbias is not None:
+        dbias, ldb = _rows_of_workers(dbias, "dbias", (n, outputs), dev)
+        pb = dbias.data_ptr()
+    py, px = dy.data_ptr(), x.data_ptr()
+    ws, need = _workspace("garfield_linear_weight_gradient_workspace", dev, py, kind, tokens,
+                          outputs, ld, px, inputs, ldx, n, counts)
+    _run("garfield_linear_weight_gradient", dev, py, kind, tokens, outputs, ld, px, inputs, ldx, n,
+         counts, out.data_ptr(), ldw, pb, ldb, ws.data_ptr() if need else None, need)
+    return out, dbias
+
+
+class ResidualNorm(NamedTuple):
+    """What residual_norm() gives: the stream s, its norm y (or None) and y's checkpoint
+    (or None), and the mean and 1 / deviation of each row (fp32): of s, and of the block's
+    result (None for a norm that is not there; no means with rms)."""
+    s: torch.Tensor
+    y: torch.Tensor | None
+    y8: Checkpoint | None
+    mean: torch.Tensor | None
+    rstd: torch.Tensor | None
+    post_mean: torch.Tensor | None
+    post_rstd: torch.Tensor | None
+
+
+def _residual_block(like: torch.Tensor, rows, cols, kind, weight, bias, post_weight, post_bias,
+                    gate, scale, eps, rms):
+    dev, dtype = like.device, like.dtype
+    wtype, pointers = None, {}
+    if rms and (bias is not None or post_bias is not None):
+        raise ValueError("with rms a norm has no bias")
+    if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
+        raise ValueError("a bias needs its weight")
+    vectors = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias}
+    if gate is not None and isinstance(gate, torch.Tensor) and gate.dim() == 1:
+        vectors["gate"] = gate
+    for name, v in vectors.items():
+        if v is not None:
+            pointers[name] = _vector(v, name, cols, _WEIGHTS[dtype] if wtype is None else (wtype,),
+                                     dev)
+            wtype = v.dtype
+    ld_gate = 0
+    if gate is not None and "gate" not in vectors:
+        pointers["gate"], ld_gate = _like(gate, "gate", rows, cols, like)
+    return _ResidualBlock(kind, TYPES[wtype or torch.float32], rows, cols, 1 if rms else 0, eps,
+                          scale, ld_gate=ld_gate, **pointers)
+
+
+def residual_norm(x: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None = None,
+                  bias: torch.Tensor | None = None, post_weight: torch.Tensor | None = None,
+                  post_bias: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                  scale: float = 1.0, eps: float = 1e-5, rms: bool = False, y: bool = True,
+                  y8: bool = False) -> ResidualNorm:
+    """The residual around a block with the norms before and after it: s = scale * x +
+    gate * N_post(h) and y = N(s), in x's type and in 8-bit blocks (y8). x: the residual stream;
+    h: the block's result. N is a layer norm of rows, with rms one by their root mean square;
+    weight None: no y, post_weight None: h as it is. gate: a value for each column, or a matrix
+    like x; weights, biases and a gate of columns are all float32 or all of x's type."""
+    rows, cols, ldx, kind = _matrix(x, "x")
+    if h is None:
+        raise ValueError("h must be a 2-D tensor (one row a token)")
+    ph, ldh = _like(h, "h", rows, cols, x)
+    dev, dtype = x.device, x.dtype
+    if cols == 0:
+        raise ValueError("x must have columns")
+    b = _residual_block(x, rows, cols, kind, weight, bias, post_weight, post_bias, gate, scale,
+                        eps, rms)
+    normed = weight is not None
+    if y8 and not normed:
+        raise ValueError("y8 needs a weight")
+    s = _empty((rows, cols), dtype=dtype, device=dev)
+    out = torch.empty_like(s) if y and normed else None
+    cy = Checkpoint.empty(rows, cols, dev) if y8 else None
+    held = [normed and not rms, normed, post_weight is not None and not rms,
+            post_weight is not None]
+    flat = iter(_empty((sum(held), rows), dtype=torch.float32, device=dev).unbind(0))
+    stats = [next(flat) if is_held else None for is_held in held]
+    _run("garfield_residual_norm", dev, _c.byref(b), x.data_ptr(), ldx, ph, ldh, s.data_ptr(),
+         cols, None if out is None else out.data_ptr(), cols,
+         *[None if v is None else v.data_ptr() for v in stats], cy._at if y8 else None)
+    return ResidualNorm(s, out, cy, *stats)
+
+
+class ResidualNormBackward(NamedTuple):
+    """What residual_norm_backward() gives: the gradients of x and h, and of each worker
+    those of the parameters that there are (n x cols, float32); dgate is that of a gate of
+    columns, or a matrix like dx for a gate like x."""
+    dx: torch.Tensor
+    dh: torch.Tensor
+    dweight: torch.Tensor | None
+    dbias: torch.Tensor | None
+    dpost_weight: torch.Tensor | None
+    dpost_bias: torch.Tensor | None
+    dgate: torch.Tensor | None
+
+
+def residual_norm_backward(r: ResidualNorm, h: torch.Tensor, ds: torch.Tensor | None = None,
+                           dy: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+                           post_weight: torch.Tensor | None = None,
+                           post_bias: torch.Tensor | None = None,
+                           gate: torch.Tensor | None = None, scale: float = 1.0,
+                           rms: bool = False, counts=None, dweight: torch.Tensor | None = None,
+                           dbias: torch.Tensor | None = None,
+                           dpost_weight: torch.Tensor | None = None,
+                           dpost_bias: torch.Tensor | None = None,
+                           dgate: torch.Tensor | None = None) -> ResidualNormBackward:
+    """The gradients of residual_norm() from that of y (dy) and what reaches s by other ways
+    (ds; one of the two may be None). r: what residual_norm() gave (s and the statistics are
+    read); h and the parameters as they were given to it; counts the tokens of each of the n
+    workers (None: one worker). dweight, dbias, dpost_weight, dpost_bias and a dgate of columns
+    (n x cols, float32) may be given, e.g. columns of the matrix of gradients. Biases have
+    gradients wherever they may have been (not with rms)."""
+    rows, cols, ldh, kind = _matrix(h, "h")
+    dev = h.device
+    if ds is None and dy is None:
+        raise ValueError("ds or dy must be given")
+    if dy is not None and weight is None:
+        raise ValueError("dy needs a weight")
+    if cols == 0:
+        raise ValueError("h must have columns")
+    b = _residual_block(h, rows, cols, kind, weight, None, post_weight, post_bias, gate, scale,
+                        0.0, rms)
+    (pds, ldds), (pdy, lddy) = _like(ds, "ds", rows, cols, h), _like(dy, "dy", rows, cols, h)
+    ps, lds = _like(r.s, "r.s", rows, cols, h)
+    stats = [None] * 4
+    for i, (name, asked) in enumerate((("mean", dy is not None and not rms),
+                                       ("rstd", dy is not None),
+                                       ("post_mean", post_weight is not None and not rms),
+                                       ("post_rstd", post_weight is not None))):
+        if asked:
+            stats[i] = _vector(getattr(r, name), "r." + name, rows, (torch.float32,), dev)
+    n, counts = _counted(counts, rows)
+    by_columns = gate is not None and gate.dim() == 1
+    if dgate is not None and not by_columns:
+        raise ValueError("dgate is given for a gate of columns only")
+    there = {"weight": (dweight, weight is not None), "bias": (dbias, weight is not None and not rms),
+             "post_weight": (dpost_weight, post_weight is not None),
+             "post_bias": (dpost_bias, post_weight is not None and not rms),
+             "gate": (dgate, by_columns)}
+    to, sums = _ResidualGradients(), {}
+    for name, (given, asked) in there.items():
+        if not asked:
+            if given is not None:
+                raise ValueError(f"d{name} was given, but there is no such parameter")
+            sums[name] = None
+            continue
+        sums[name], ld = _rows_of_workers(given, "d" + name, (n, cols), dev)
+        setattr(to, name, sums[name].data_ptr())
+        setattr(to, "ld_" + name, ld)
+    dx = _empty((rows, cols), dtype=h.dtype, device=dev)
+    dh = torch.empty_like(dx)
+    by_tokens = gate is not None and not by_columns
+    dg = torch.empty_like(dx) if by_tokens else None
+    at = _c.byref(b)
+    ws, need = _workspace("garfield_residual_norm_backward_workspace", dev, at, n, counts)
+    _run("garfield_residual_norm_backward", dev, at, pds, ldds, pdy, lddy, ps, lds, h.data_ptr(),
+         ldh, *stats, dx.data_ptr(), cols, dh.data_ptr(), cols, dg.data_ptr() if by_tokens else None,
+         cols, n, counts, _c.byref(to), ws.data_ptr() if need else None, need)
+    return ResidualNormBackward(dx, dh, sums["weight"], sums["bias"], sums["post_weight"],
+                                sums["post_bias"], dg if by_tokens else sums["gate"])
+
+
+def _tensors(grads):
+    """The workers' tensors as garfield_clip_gradients takes them: their count, the workers,
+    the C array, the device and the values of a worker."""
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
+    if not grads:
+        raise ValueError("grads must hold a tensor")
+    held = (_Gradient * len(grads))()
+    n, dev, d = None, None, 0
+    for i, g in enumerate(grads):
+        if not isinstance(g, torch.Tensor) or g.dim() < 1 or g.dtype not in TYPES or not g.is_cuda:
+            raise ValueError("grads must be float32, bfloat16 or float16 tensors on a GPU, "
+                             "their first dimension the workers")
+        n, dev = (g.shape[0], g.device) if n is None else (n, dev)
+        if g.shape[0] != n or g.device != dev or n < 1:
+            raise ValueError("grads must have the same workers (one at least) and device")
+        length, ld = g.numel() // n, g.stride(0)
+        if n == 1:
+            ld = length
+        if length and not (g.is_contiguous() or (g[0].is_contiguous() and ld >= length)):
+            raise ValueError("each worker's values of a tensor must be next to each other, and "
+                             "the workers' must not overlap")
+        held[i] = _Gradient(g.data_ptr(), length, ld, TYPES[g.dtype])
+        d += length
+    return len(grads), n, held, dev, d
+
+
+def gradient_norms(grads) -> torch.Tensor:
+    """The norm of each worker's gradient over all its tensors (float32). grads: tensors of
+    any types and shapes whose first dimension is the workers, e.g. n x d or n x outputs x
+    inputs (a list, or one tensor)."""
+    count, n, held, dev, _ = _tensors(grads)
+    norms = _empty(n, dtype=torch.float32, device=dev)
+    ws, need = _workspace("garfield_clip_workspace", dev, held, count, n)
+    _run("garfield_gradient_norms", dev, held, count, n, norms.data_ptr(),
+         ws.data_ptr() if need else None, need)
+    return norms
+
+
+def clip_gradients(grads, max_norm: float, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Clip each worker's gradient to max_norm: all its tensors' values times max_norm / norm
+    where its norm over all of them is larger. In place, or with out (n x d, float32) the
+    tensors one after the other into the workers' rows of out, e.g. the matrix that the rules
+    take. Returns the norms before (float32). grads as for gradient_norms()."""
+    count, n, held, dev, d = _tensors(grads)
+    if not max_norm >= 0:
+        raise ValueError("max_norm must be 0 or more")
+    po, ld = None, 0
+    if out is not None:
+        out, ld = _rows_of_workers(out, "out", (n, d), dev)
+        po = out.data_ptr()
+    norms = _empty(n, dtype=torch.float32, device=dev)
+    ws, need = _workspace("garfield_clip_workspace", dev, held, count, n)
+    _run("garfield_clip_gradients", dev, held, count, n, max_norm, norms.data_ptr(), po, ld,
+         ws.data_ptr() if need else None, need)
+    return norms
