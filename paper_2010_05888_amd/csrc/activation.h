@@ -23,31 +23,64 @@ __device__ __forceinline__ float normal_below(float p) {
   return 0.5f * erfcf(-0.70710678118654752f * p);
 }
 
-__device__ __forceinline__ float activate(int activation, float p) {
+// N values at a time, for one decision.
+template <int N>
+__device__ __forceinline__ void activate(int activation, float* v) {
   switch (activation) {
-    case GARFIELD_RELU: return p < 0.0f ? 0.0f : p;  // NaN stays
-    case GARFIELD_GELU: return p * normal_below(p);
-    case GARFIELD_GELU_TANH: return p * logistic(tanh_argument(p));
-    case GARFIELD_SILU: return p * logistic(p);
-    default: return p;
+    case GARFIELD_RELU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = v[e] < 0.0f ? 0.0f : v[e];  // NaN stays
+      break;
+    case GARFIELD_GELU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= normal_below(v[e]);
+      break;
+    case GARFIELD_GELU_TANH:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= logistic(tanh_argument(v[e]));
+      break;
+    case GARFIELD_SILU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= logistic(v[e]);
+      break;
+    default: break;
   }
 }
 
-__device__ __forceinline__ float slope(int activation, float p) {
+__device__ __forceinline__ float gelu_slope(float p) {
+  return __builtin_fmaf(p * 0.39894228040143268f, expf(-0.5f * p * p), normal_below(p));
+}
+
+__device__ __forceinline__ float gelu_tanh_slope(float p) {
+  const float u = tanh_argument(p), q = logistic(u), rest = q * logistic(-u);
+  const float du = kTanhScale * __builtin_fmaf(3.0f * kTanhCube * p, p, 1.0f);
+  return rest == 0.0f ? q : __builtin_fmaf(p * rest, du, q);  // du may be infinite
+}
+
+// v times the slopes at p.
+template <int N>
+__device__ __forceinline__ void times_slope(int activation, const float* p, float* v) {
   switch (activation) {
-    case GARFIELD_RELU: return p > 0.0f ? 1.0f : 0.0f;
+    case GARFIELD_RELU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= p[e] > 0.0f ? 1.0f : 0.0f;
+      break;
     case GARFIELD_GELU:
-      return __builtin_fmaf(p * 0.39894228040143268f, expf(-0.5f * p * p), normal_below(p));
-    case GARFIELD_GELU_TANH: {
-      const float u = tanh_argument(p), q = logistic(u), rest = q * logistic(-u);
-      const float du = kTanhScale * __builtin_fmaf(3.0f * kTanhCube * p, p, 1.0f);
-      return rest == 0.0f ? q : __builtin_fmaf(p * rest, du, q);  // du may be infinite
-    }
-    case GARFIELD_SILU: {
-      const float q = logistic(p);
-      return q * __builtin_fmaf(p, logistic(-p), 1.0f);
-    }
-    default: return 1.0f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= gelu_slope(p[e]);
+      break;
+    case GARFIELD_GELU_TANH:
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= gelu_tanh_slope(p[e]);
+      break;
+    case GARFIELD_SILU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float q = logistic(p[e]);
+        v[e] *= q * __builtin_fmaf(p[e], logistic(-p[e]), 1.0f);
+      }
+      break;
+    default: break;
   }
 }
 
