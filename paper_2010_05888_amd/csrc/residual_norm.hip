@@ -3,24 +3,13 @@
 
 #include "block8.h"
 #include "internal.h"
+#include "row_sums.h"
 #include "timing.h"
 #include "worker.h"
 
 namespace garfield {
 
 namespace {
-
-template <typename F>
-__device__ __forceinline__ F sum_group(F v, F* at) {
-  v = sum_wave(v);
-  __syncthreads();  // the last sum has been read
-  if (threadIdx.x % 64 == 0) at[threadIdx.x / 64] = v;
-  __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < kBlock / 64; ++w) v += at[w];
-  return v;
-}
 
 template <typename T>
 __device__ __forceinline__ void load_parameter(const void* p, bool f32, int64_t c, int64_t left,
@@ -72,38 +61,199 @@ __device__ __forceinline__ void stream_values(const ResidualNorm& a, int64_t row
   for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(a.b.scale, v[e], g[e] * f[e]);
 }
 
+constexpr int kLong = 1024, kLongWaves = kLong / 64;  // threads to a row that is read again and again
+
 // Mean (0 with rms) and 1 / deviation of a row, `values` giving eight columns of it.
 template <typename F>
-__device__ __forceinline__ void statistics(const garfield_residual_block& b, double share,
+__device__ __forceinline__ void long_statistics(const garfield_residual_block& b, double share,
                                            double* totals, float* sums, F&& values, float* mean,
                                            float* rstd) {
   float v[8];
   *mean = 0.0f;
   if (!b.rms) {
     double sum = 0.0;
-    for (int64_t c = threadIdx.x * 8; c < b.cols; c += kBlock * 8) {
+    for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
       values(c, v);
       for (int e = 0; e < 8 && c + e < b.cols; ++e) sum += v[e];
     }
-    *mean = static_cast<float>(sum_group(sum, totals) * share);
+    *mean = static_cast<float>(sum_group<kLongWaves>(sum, totals) * share);
   }
   float square = 0.0f;
-  for (int64_t c = threadIdx.x * 8; c < b.cols; c += kBlock * 8) {
+  for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
     values(c, v);
     for (int e = 0; e < 8 && c + e < b.cols; ++e)
       square = __builtin_fmaf(v[e] - *mean, v[e] - *mean, square);
   }
-  *rstd = 1.0f / __builtin_sqrtf(sum_group(square, sums) * static_cast<float>(share) + b.eps);
+  square = sum_group<kLongWaves>(square, sums);
+  *rstd = 1.0f / __builtin_sqrtf(square * static_cast<float>(share) + b.eps);
 }
 
+// Mean (0 with rms) and 1 / deviation of R rows that a team of WAVES waves holds, NV vectors of
+// eight columns of each to a lane: values(r, j, v) gives them.
+template <int WAVES, int NV, int R, typename F>
+__device__ __forceinline__ void statistics(const garfield_residual_block& b, double share, int lane,
+                                           double (*totals)[R], float (*sums)[R], F&& values,
+                                           float* mean, float* rstd) {
+  constexpr int kThreads = 64 * WAVES;
+  const int cols = static_cast<int>(b.cols);
+  float v[8];
+  if (b.rms) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) mean[r] = 0.0f;
+  } else {
+    double total[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float sum = 0.0f, first = 0.0f;
+      int count = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int left = cols - (j * kThreads + lane) * 8;
+        values(r, j, v);
+        if (j == 0) first = first_value(v[0]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += left >= 8 || e < left ? v[e] - first : 0.0f;
+        count += left >= 8 ? 8 : left > 0 ? left : 0;
+      }
+      total[r] = lane_total(first, count, sum);
+    }
+    sums_group<WAVES, R>(total, totals);
+#pragma unroll
+    for (int r = 0; r < R; ++r) mean[r] = static_cast<float>(total[r] * share);
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float square = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int left = cols - (j * kThreads + lane) * 8;
+      values(r, j, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float t = left >= 8 || e < left ? v[e] - mean[r] : 0.0f;
+        square = __builtin_fmaf(t, t, square);
+      }
+    }
+    rstd[r] = square;
+  }
+  sums_group<WAVES, R>(rstd, sums);
+  const float scale = static_cast<float>(share);
+#pragma unroll
+  for (int r = 0; r < R; ++r) rstd[r] = 1.0f / __builtin_sqrtf(rstd[r] * scale + b.eps);
+}
+
+// Rows of up to 512 * WAVES * NV columns, R rows at a time to a team of WAVES waves; workgroups
+// of four waves hold 4 / WAVES teams. x and h are read once; the stream stays in registers in
+// fp32 from its sum to its norm. Several rows at a time share the parameters' reads.
+template <typename T, int WAVES, int NV, int R>
+__global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void k_residual_norm(ResidualNorm a) {
+  constexpr int kThreads = 64 * WAVES;
+  constexpr int kTeams = WAVES > 4 ? 1 : 4 / WAVES;
+  static_assert(WAVES == 1 || kTeams == 1, "barriers are the whole workgroup's");
+  __shared__ double totals[2][WAVES][R];
+  __shared__ float sums[2][WAVES][R];
+  const garfield_residual_block& b = a.b;
+  const int64_t row0 = (static_cast<int64_t>(blockIdx.x) * kTeams + threadIdx.x / kThreads) * R;
+  if (row0 >= b.rows) return;  // whole waves, and no barrier where there are several teams
+  const int lane = threadIdx.x % kThreads;
+  const bool f32 = b.wtype == GARFIELD_F32, by_tokens = b.gate && b.ld_gate;
+  typedef typename Pack8<T>::type Raw;
+  Raw x[R][NV], h[R][NV], gate[R][NV];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = row0 + r < b.rows ? row0 + r : b.rows - 1;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * kThreads + lane) * 8;
+      h[r][j] = raw8_upto(static_cast<const T*>(a.h) + row * a.ldh + c, b.cols - c);
+      x[r][j] = raw8_upto(static_cast<const T*>(a.x) + row * a.ldx + c, b.cols - c);
+      if (by_tokens) gate[r][j] = raw8_upto(static_cast<const T*>(b.gate) + row * b.ld_gate + c, b.cols - c);
+    }
+  }
+  float mean[R], rstd[R], s[R][NV][8];
+  if (b.post_weight) {
+    statistics<WAVES, NV, R>(b, a.share, lane, totals[0], sums[0],
+                             [&](int r, int j, float* v) { unpack8<T>(h[r][j], v); }, mean, rstd);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (lane == 0 && row0 + r < b.rows) {
+        if (!b.rms) a.post_mean[row0 + r] = mean[r];
+        a.post_rstd[row0 + r] = rstd[r];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int64_t c = (j * kThreads + lane) * 8, left = b.cols - c;
+    float w[8], bias[8], g[8], t[8];
+    if (b.post_weight) {
+      load_weight<T>(b.post_weight, f32, c, left, w);
+      load_parameter<T>(b.post_bias, f32, c, left, 0.0f, bias);
+    }
+    if (!by_tokens) load_parameter<T>(b.gate, f32, c, left, 1.0f, g);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float* v = s[r][j];
+      unpack8<T>(h[r][j], v);
+      unpack8<T>(x[r][j], t);
+      if (b.post_weight) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = __builtin_fmaf((v[e] - mean[r]) * rstd[r], w[e], bias[e]);
+      }
+      if (by_tokens) unpack8<T>(gate[r][j], g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(b.scale, t[e], g[e] * v[e]);
+      if (row0 + r < b.rows)
+        store8_upto(static_cast<T*>(a.s) + (row0 + r) * a.lds + c, left, v);
+    }
+  }
+  if (!b.weight) return;
+  statistics<WAVES, NV, R>(b, a.share, lane, totals[1], sums[1],
+                           [&](int r, int j, float* v) {
+#pragma unroll
+                             for (int e = 0; e < 8; ++e) v[e] = s[r][j][e];
+                           },
+                           mean, rstd);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (lane == 0 && row0 + r < b.rows) {
+      if (!b.rms) a.mean[row0 + r] = mean[r];
+      a.rstd[row0 + r] = rstd[r];
+    }
+  }
+  if (!a.y && !a.y8.values) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int64_t c = (j * kThreads + lane) * 8, left = b.cols - c;
+    float w[8], bias[8];
+    load_weight<T>(b.weight, f32, c, left, w);
+    load_parameter<T>(b.bias, f32, c, left, 0.0f, bias);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = row0 + r;
+      if (row >= b.rows) break;
+      float* v = s[r][j];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = __builtin_fmaf((v[e] - mean[r]) * rstd[r], w[e], bias[e]);
+        if (left < 8) v[e] = e < left ? v[e] : 0.0f;
+      }
+      if (a.y) store8_upto(static_cast<T*>(a.y) + row * a.ldy + c, left, v);
+      if (a.y8.values) store_blocks(a.y8, row, c, v);
+    }
+  }
+}
+
+// Longer rows: the workgroup reads them again for each of its sums.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_residual_norm(ResidualNorm a) {
-  __shared__ double totals[kBlock / 64];
-  __shared__ float sums[kBlock / 64];
+__global__ __launch_bounds__(kLong) void k_residual_norm_long(ResidualNorm a) {
+  __shared__ double totals[2][kLongWaves];
+  __shared__ float sums[2][kLongWaves];
   const int64_t row = blockIdx.x;
   float pm = 0.0f, pr = 1.0f, mean, rstd, v[8];
   if (a.b.post_weight) {
-    statistics(a.b, a.share, totals, sums, [&](int64_t c, float* h) {
+    long_statistics(a.b, a.share, totals[0], sums[0], [&](int64_t c, float* h) {
       load8_upto(static_cast<const T*>(a.h) + row * a.ldh + c, a.b.cols - c, h);
     }, &pm, &pr);
     if (threadIdx.x == 0) {
@@ -113,7 +263,7 @@ __global__ __launch_bounds__(kBlock) void k_residual_norm(ResidualNorm a) {
   }
   auto values = [&](int64_t c, float* t) { stream_values<T>(a, row, c, pm, pr, t); };
   if (a.b.weight) {
-    statistics(a.b, a.share, totals, sums, values, &mean, &rstd);
+    long_statistics(a.b, a.share, totals[1], sums[1], values, &mean, &rstd);
     if (threadIdx.x == 0) {
       if (!a.b.rms) a.mean[row] = mean;
       a.rstd[row] = rstd;
@@ -121,7 +271,7 @@ __global__ __launch_bounds__(kBlock) void k_residual_norm(ResidualNorm a) {
   }
   const bool f32 = a.b.wtype == GARFIELD_F32;
   const int64_t padded = (a.b.cols + 511) / 512 * 512;
-  for (int64_t c = threadIdx.x * 8; c < padded; c += kBlock * 8) {
+  for (int64_t c = threadIdx.x * 8; c < padded; c += kLong * 8) {
     const int64_t left = a.b.cols - c;
     float w[8], bias[8];
     if (left > 0) {
@@ -135,14 +285,7 @@ __global__ __launch_bounds__(kBlock) void k_residual_norm(ResidualNorm a) {
     for (int e = 0; e < 8; ++e)
       v[e] = e < left ? __builtin_fmaf((v[e] - mean) * rstd, w[e], bias[e]) : 0.0f;
     if (a.y && left > 0) store8_upto(static_cast<T*>(a.y) + row * a.ldy + c, left, v);
-    if (a.y8.values) {
-      const int s = block_shift(max16(largest<8>(v)));
-      const int64_t blocks = (a.y8.cols + kBlock8 - 1) / kBlock8, k = c / kBlock8;
-      if (k < blocks)
-        *reinterpret_cast<u2*>(a.y8.values + row * a.y8.ld_values + c) = encode8(v, s);
-      if (c % kBlock8 == 0 && k < (blocks + 3) / 4 * 4)
-        a.y8.exponents[row * a.y8.ld_exponents + k] = static_cast<uint8_t>(k < blocks ? s + 127 : 127);
-    }
+    if (a.y8.values) store_blocks(a.y8, row, c, v);
   }
 }
 
@@ -184,11 +327,12 @@ __device__ __forceinline__ void backward_values(const ResidualNormBackward& a, i
 // The means over a row of dy w (0 with rms) and dy w hat.
 template <typename T>
 __device__ __forceinline__ void backward_sums(const ResidualNormBackward& a, int64_t row,
-                                              float* sums, float* along, float* across) {
+                                              float (*sums)[kLongWaves], float* along,
+                                              float* across) {
   const garfield_residual_block& b = a.b;
   float x = 0.0f, y = 0.0f, w[8];
   Eight t;
-  for (int64_t c = threadIdx.x * 8; c < b.cols; c += kBlock * 8) {
+  for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
     backward_values<T>(a, row, c, 0.0f, 0.0f, t);
     load_parameter<T>(b.weight, b.wtype == GARFIELD_F32, c, b.cols - c, 1.0f, w);
     for (int e = 0; e < 8 && c + e < b.cols; ++e) {
@@ -197,13 +341,14 @@ __device__ __forceinline__ void backward_sums(const ResidualNormBackward& a, int
     }
   }
   const float cols = static_cast<float>(b.cols);
-  *along = b.rms ? 0.0f : sum_group(x, sums) / cols;
-  *across = sum_group(y, sums) / cols;
+  x = sum_group<kLongWaves>(x, sums[0]) / cols;
+  *along = b.rms ? 0.0f : x;
+  *across = sum_group<kLongWaves>(y, sums[1]) / cols;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_residual_dx(ResidualNormBackward a, float2* means) {
-  __shared__ float sums[kBlock / 64];
+__global__ __launch_bounds__(kLong) void k_residual_dx_long(ResidualNormBackward a, float2* means) {
+  __shared__ float sums[4][kLongWaves];
   const garfield_residual_block& b = a.b;
   const int64_t row = blockIdx.x;
   float along = 0.0f, across = 0.0f, w[8];
@@ -213,7 +358,7 @@ __global__ __launch_bounds__(kBlock) void k_residual_dx(ResidualNormBackward a, 
   Eight t;
   const bool f32 = b.wtype == GARFIELD_F32;
   if (b.post_weight) {
-    for (int64_t c = threadIdx.x * 8; c < b.cols; c += kBlock * 8) {
+    for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
       backward_values<T>(a, row, c, along, across, t);
       load_parameter<T>(b.post_weight, f32, c, b.cols - c, 1.0f, w);
       for (int e = 0; e < 8 && c + e < b.cols; ++e) {
@@ -222,11 +367,12 @@ __global__ __launch_bounds__(kBlock) void k_residual_dx(ResidualNormBackward a, 
       }
     }
     const float cols = static_cast<float>(b.cols);
-    x = b.rms ? 0.0f : sum_group(x, sums) / cols;
-    y = sum_group(y, sums) / cols;
+    x = sum_group<kLongWaves>(x, sums[2]) / cols;
+    x = b.rms ? 0.0f : x;
+    y = sum_group<kLongWaves>(y, sums[3]) / cols;
   }
   const float pr = b.post_weight ? a.post_rstd[row] : 1.0f;
-  for (int64_t c = threadIdx.x * 8; c < b.cols; c += kBlock * 8) {
+  for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
     const int64_t left = b.cols - c;
     backward_values<T>(a, row, c, along, across, t);
     load_parameter<T>(b.post_weight, f32, c, left, 1.0f, w);
@@ -242,14 +388,216 @@ __global__ __launch_bounds__(kBlock) void k_residual_dx(ResidualNormBackward a, 
   }
 }
 
-// partial[chunk][5][cols]
+// A worker's sums over its rows: weight, bias, post weight, post bias, gate; `sums` has a bit
+// for each that is asked for, and partial[chunk][bit's rank][cols] a chunk's.
 constexpr int kSums = 5;
+
+// A workgroup goes through one chunk of a worker's rows (up to 8 * THREADS * NV columns), its
+// share of the parameters' gradients in registers, and writes that to `partial`;
+// k_residual_sums adds the chunks of a worker. R rows are worked on at a time, with one
+// barrier for each norm's sums, while the next R are on their way.
+// HOLD: the parameters stay in registers, else they are read again for every R rows.
+template <typename T, int THREADS, int NV, int R, bool HOLD>
+__global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackward a,
+                                                               Chunks chunks, int sums_of,
+                                                               float* partial) {
+  constexpr int kWaves = THREADS / 64;
+  typedef typename Pack8<T>::type Raw;
+  __shared__ float sums[2][2][kWaves][2 * R];
+  const garfield_residual_block& b = a.b;
+  const int chunk = blockIdx.x, worker = worker_of(chunks, chunk);
+  const int64_t begin = chunks.token0[worker] + (chunk - chunks.chunk0[worker]) * chunks.rows;
+  const int64_t last = chunks.token0[worker + 1];
+  const int64_t end = begin + chunks.rows < last ? begin + chunks.rows : last;
+  const float scale = 1.0f / static_cast<float>(b.cols);
+  const bool f32 = b.wtype == GARFIELD_F32, by_tokens = b.gate && b.ld_gate;
+  const bool post = b.post_weight != nullptr;
+  float w[NV][8], pw[NV][8], pb[NV][8], gv[NV][8], total[kSums][NV][8];
+  auto parameter = [&](const void* p, float missing, float (&v)[NV][8]) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * THREADS + threadIdx.x) * 8;
+      load_parameter<T>(p, f32, c, b.cols - c, missing, v[j]);
+    }
+  };
+  const void* const columns = by_tokens ? nullptr : b.gate;
+  if constexpr (HOLD) {
+    parameter(b.weight, 0.0f, w);
+    parameter(b.post_weight, 1.0f, pw);
+    parameter(b.post_bias, 0.0f, pb);
+    parameter(columns, 1.0f, gv);
+  }
+#pragma unroll
+  for (int k = 0; k < kSums; ++k)
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) total[k][j][e] = 0.0f;
+  Raw ds[R][NV], dy[R][NV], s[R][NV], h[R][NV], gate[R][NV];
+  float mean[R], rstd[R], post_mean[R], post_rstd[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    mean[r] = post_mean[r] = 0.0f;
+    rstd[r] = post_rstd[r] = 1.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ds[r][j][e] = dy[r][j][e] = s[r][j][e] = static_cast<T>(0.0f);
+  }
+  auto fetch = [&](int64_t row0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = row0 + r < end ? row0 + r : end - 1;
+      if (a.dy) {
+        if (!b.rms) mean[r] = a.mean[row];
+        rstd[r] = a.rstd[row];
+      }
+      if (post) {
+        if (!b.rms) post_mean[r] = a.post_mean[row];
+        post_rstd[r] = a.post_rstd[row];
+      }
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+        auto of = [&](const void* p, int64_t ld) {
+          return raw8_upto(static_cast<const T*>(p) + row * ld + c, left);
+        };
+        if (a.dy) {
+          dy[r][j] = of(a.dy, a.lddy);
+          s[r][j] = of(a.s, a.lds);
+        }
+        if (a.ds) ds[r][j] = of(a.ds, a.ldds);
+        h[r][j] = of(a.h, a.ldh);
+        if (by_tokens) gate[r][j] = of(b.gate, b.ld_gate);
+      }
+    }
+  };
+  fetch(begin);
+  for (int64_t row0 = begin; row0 < end; row0 += R) {
+    const int odd = (row0 - begin) / R & 1;  // the sums alternate between two places
+    float g[R][NV][8], hat[R][NV][8], z[R][NV][8], k[R][NV][8], both[2 * R], d[R], pd[R];
+    if constexpr (!HOLD) {
+      parameter(b.weight, 0.0f, w);
+      parameter(columns, 1.0f, gv);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool there = r == 0 || row0 + r < end;
+      float along = 0.0f, across = 0.0f;
+      d[r] = rstd[r];
+      pd[r] = post_rstd[r];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int64_t left = b.cols - (j * THREADS + threadIdx.x) * 8;
+        unpack8<T>(dy[r][j], g[r][j]);
+        unpack8<T>(s[r][j], hat[r][j]);
+        unpack8<T>(h[r][j], z[r][j]);
+        if (by_tokens) unpack8<T>(gate[r][j], k[r][j]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (!by_tokens) k[r][j][e] = gv[j][e];
+          hat[r][j][e] = (hat[r][j][e] - mean[r]) * d[r];
+          if (post) z[r][j][e] = (z[r][j][e] - post_mean[r]) * pd[r];
+          if (left < 8 && e >= left) hat[r][j][e] = z[r][j][e] = 0.0f;
+          if (there) {
+            total[0][j][e] = __builtin_fmaf(g[r][j][e], hat[r][j][e], total[0][j][e]);
+            total[1][j][e] += g[r][j][e];
+          }
+          g[r][j][e] *= w[j][e];
+          along += g[r][j][e];
+          across = __builtin_fmaf(g[r][j][e], hat[r][j][e], across);
+        }
+      }
+      both[2 * r] = along;
+      both[2 * r + 1] = across;
+    }
+    // ds goes on to the whole gradient, and the next rows come
+    float more[R][NV][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) unpack8<T>(ds[r][j], more[r][j]);
+    if (row0 + R < end) fetch(row0 + R);
+    if (a.dy) sums_group<kWaves, 2 * R>(both, sums[0][odd]);
+    if constexpr (!HOLD) {
+      parameter(b.post_weight, 1.0f, pw);
+      parameter(b.post_bias, 0.0f, pb);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool there = r == 0 || row0 + r < end;
+      const float along = b.rms || !a.dy ? 0.0f : both[2 * r] * scale;
+      const float across = a.dy ? both[2 * r + 1] * scale : 0.0f;
+      float x = 0.0f, y = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float v = more[r][j][e];
+          if (a.dy) v += d[r] * (g[r][j][e] - along - hat[r][j][e] * across);
+          if (left < 8 && e >= left) v = 0.0f;
+          g[r][j][e] = v;
+          f[e] = post ? __builtin_fmaf(z[r][j][e], pw[j][e], pb[j][e]) : z[r][j][e];
+          f[e] *= v;
+          k[r][j][e] *= v;  // the gradient of N_post(h)
+          if (there) {
+            total[2][j][e] = __builtin_fmaf(k[r][j][e], z[r][j][e], total[2][j][e]);
+            total[3][j][e] += k[r][j][e];
+            total[4][j][e] += f[e];
+          }
+          if (post) {
+            k[r][j][e] *= pw[j][e];
+            x += k[r][j][e];
+            y = __builtin_fmaf(k[r][j][e], z[r][j][e], y);
+          }
+          g[r][j][e] *= b.scale;
+        }
+        if (there && left > 0) {
+          if (a.dx) store8_upto(static_cast<T*>(a.dx) + (row0 + r) * a.lddx + c, left, g[r][j]);
+          if (a.dgate) store8_upto(static_cast<T*>(a.dgate) + (row0 + r) * a.lddgate + c, left, f);
+        }
+      }
+      both[2 * r] = x;
+      both[2 * r + 1] = y;
+    }
+    if (!a.dh) continue;
+    if (post) sums_group<kWaves, 2 * R>(both, sums[1][odd]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r > 0 && row0 + r >= end) break;
+      const float x = b.rms ? 0.0f : both[2 * r] * scale, y = both[2 * r + 1] * scale;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+        if (post) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) k[r][j][e] = pd[r] * (k[r][j][e] - x - z[r][j][e] * y);
+        }
+        if (left > 0) store8_upto(static_cast<T*>(a.dh) + (row0 + r) * a.lddh + c, left, k[r][j]);
+      }
+    }
+  }
+  int rank = 0;
+  const int asked = __builtin_popcount(sums_of);
+#pragma unroll
+  for (int q = 0; q < kSums; ++q) {
+    if (!(sums_of >> q & 1)) continue;
+    float* out = partial + (static_cast<int64_t>(chunk) * asked + rank++) * b.cols;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * THREADS + threadIdx.x) * 8;
+      if (c < b.cols) store8_upto(out + c, b.cols - c, total[q][j]);
+    }
+  }
+}
+
 template <typename T>
-__global__ __launch_bounds__(64) void k_residual_dw(ResidualNormBackward a, Chunks chunks,
-                                                    const float2* means, float* partial) {
-  const int chunk = blockIdx.y;
-  int worker = 0;
-  while (chunks.chunk0[worker + 1] <= chunk) ++worker;
+__global__ __launch_bounds__(64) void k_residual_dw_long(ResidualNormBackward a, Chunks chunks,
+                                                         const float2* means, int sums_of,
+                                                         float* partial) {
+  const int chunk = blockIdx.y, worker = worker_of(chunks, chunk);
   const int64_t begin = chunks.token0[worker] + (chunk - chunks.chunk0[worker]) * chunks.rows;
   const int64_t last = chunks.token0[worker + 1];
   const int64_t end = begin + chunks.rows < last ? begin + chunks.rows : last;
@@ -269,73 +617,157 @@ __global__ __launch_bounds__(64) void k_residual_dw(ResidualNormBackward a, Chun
       sum[4][e] = __builtin_fmaf(t.g[e], t.f[e], sum[4][e]);
     }
   }
-  for (int k = 0; k < kSums; ++k)
-    store8_upto(partial + (static_cast<int64_t>(chunk) * kSums + k) * a.b.cols + c, a.b.cols - c,
-                sum[k]);
+  int rank = 0;
+  const int asked = __builtin_popcount(sums_of);
+#pragma unroll
+  for (int q = 0; q < kSums; ++q)
+    if (sums_of >> q & 1)
+      store8_upto(partial + (static_cast<int64_t>(chunk) * asked + rank++) * a.b.cols + c,
+                  a.b.cols - c, sum[q]);
 }
 
+// The chunks of a worker added in one order: 64 columns of one of the sums at a time for
+// worker blockIdx.y, every fourth chunk to a wave.
 __global__ __launch_bounds__(kBlock) void k_residual_sums(const float* __restrict__ partial,
-                                                          int64_t cols, Chunks chunks,
+                                                          int64_t cols, Chunks chunks, int sums_of,
                                                           garfield_residual_gradients to) {
-  const int k = blockIdx.y % kSums, worker = blockIdx.y / kSums;
-  float* const outs[kSums] = {to.weight, to.bias, to.post_weight, to.post_bias, to.gate};
-  const int64_t lds[kSums] = {to.ld_weight, to.ld_bias, to.ld_post_weight, to.ld_post_bias, to.ld_gate};
-  if (!outs[k]) return;
-  for (int64_t c = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; c < cols;
-       c += static_cast<int64_t>(gridDim.x) * kBlock) {
+  __shared__ float sums[4][64];
+  const int asked = __builtin_popcount(sums_of);
+  const int lane = threadIdx.x % 64, part = threadIdx.x / 64, worker = blockIdx.y;
+  const int64_t groups = (cols + 63) / 64;
+  for (int64_t i = blockIdx.x; i < groups * asked; i += gridDim.x) {
+    const int rank = static_cast<int>(i / groups);
+    const int64_t c = i % groups * 64 + lane;
     float sum = 0.0f;
-    for (int i = chunks.chunk0[worker]; i < chunks.chunk0[worker + 1]; ++i)
-      sum += partial[(static_cast<int64_t>(i) * kSums + k) * cols + c];
-    outs[k][worker * lds[k] + c] = sum;
+    if (c < cols) {
+#pragma unroll 8
+      for (int k = chunks.chunk0[worker] + part; k < chunks.chunk0[worker + 1]; k += 4)
+        sum += partial[(static_cast<int64_t>(k) * asked + rank) * cols + c];
+    }
+    sums[part][lane] = sum;
+    __syncthreads();
+    if (part == 0 && c < cols) {
+      sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+      int q = 0;
+      for (int left = rank; left >= 0; ++q) left -= sums_of >> q & 1;
+      float* const outs[kSums] = {to.weight, to.bias, to.post_weight, to.post_bias, to.gate};
+      const int64_t lds[kSums] = {to.ld_weight, to.ld_bias, to.ld_post_weight, to.ld_post_bias,
+                                  to.ld_gate};
+#pragma unroll
+      for (int k = 0; k < kSums; ++k)
+        if (k == q - 1) outs[k][worker * lds[k] + c] = sum;
+    }
+    __syncthreads();  // the sums' places are free
   }
+}
+
+int sums_asked(const garfield_residual_gradients& to) {
+  return (to.weight ? 1 : 0) | (to.bias ? 2 : 0) | (to.post_weight ? 4 : 0) |
+         (to.post_bias ? 8 : 0) | (to.gate ? 16 : 0);
+}
+
+constexpr int64_t kBackwardMaxCols = 8192;
+
+template <typename T, int THREADS, int NV, int R, bool HOLD = true>
+void launch_backward(const ResidualNormBackward& a, const Chunks& c, float* partial, hipStream_t s) {
+  launch("residual_backward", k_residual_backward<T, THREADS, NV, R, HOLD>, dim3(c.chunk0[c.n]),
+         dim3(THREADS), 0, s, a, c, sums_asked(a.to), partial);
 }
 
 template <typename T>
-void launch_backward(const ResidualNormBackward& a, const Chunks& c, void* workspace, hipStream_t s) {
+void choose_backward(const ResidualNormBackward& a, const Chunks& c, void* workspace, hipStream_t s) {
   float2* means = static_cast<float2*>(workspace);
-  float* partial = reinterpret_cast<float*>(means + a.b.rows);
-  const garfield_residual_gradients& to = a.to;
-  const bool sums = to.weight || to.bias || to.post_weight || to.post_bias || to.gate;
+  const int64_t cols = a.b.cols;
+  float* partial = reinterpret_cast<float*>(cols > kBackwardMaxCols ? means + a.b.rows : means);
+  const int sums = sums_asked(a.to);
   if (a.b.rows > 0) {
-    launch("residual_dx", k_residual_dx<T>, dim3(static_cast<uint32_t>(a.b.rows)), dim3(kBlock), 0,
-           s, a, means);
-    if (sums)
-      launch("residual_dw", k_residual_dw<T>,
-             dim3(static_cast<uint32_t>((a.b.cols + 511) / 512), c.chunk0[c.n]), dim3(64), 0, s, a,
-             c, means, partial);
+    if (cols > kBackwardMaxCols) {
+      launch("residual_dx_long", k_residual_dx_long<T>, dim3(static_cast<uint32_t>(a.b.rows)),
+             dim3(kLong), 0, s, a, means);
+      if (sums)
+        launch("residual_dw_long", k_residual_dw_long<T>,
+               dim3(static_cast<uint32_t>((cols + 511) / 512), c.chunk0[c.n]), dim3(64), 0, s, a, c,
+               means, sums, partial);
+    } else if (cols > 4096) {
+      launch_backward<T, 1024, 1, 1, false>(a, c, partial, s);
+    } else if (cols > 2048) {
+      launch_backward<T, 512, 1, 1>(a, c, partial, s);
+    } else if (cols > 1024) {
+      launch_backward<T, 256, 1, 1>(a, c, partial, s);
+    } else if (cols > 512) {
+      launch_backward<T, 128, 1, 1>(a, c, partial, s);
+    } else {
+      launch_backward<T, 64, 1, 1>(a, c, partial, s);
+    }
   }
   if (sums) {
-    const int64_t groups = (a.b.cols + kBlock - 1) / kBlock, most = int64_t{1} << 15;
+    // a workgroup for 64 columns, up to 2^17 of them a worker: a launch has fewer than 2^32 threads
+    const int64_t groups = (cols + 63) / 64 * __builtin_popcount(sums), most = int64_t{1} << 17;
     launch("residual_sums", k_residual_sums,
-           dim3(static_cast<uint32_t>(groups < most ? groups : most), c.n * kSums), dim3(kBlock), 0,
-           s, partial, a.b.cols, c, to);
+           dim3(static_cast<uint32_t>(groups < most ? groups : most), c.n), dim3(kBlock), 0, s,
+           partial, cols, c, sums, a.to);
   }
+}
+
+template <typename T, int WAVES, int NV, int R>
+void launch_forward(const ResidualNorm& a, hipStream_t s) {
+  constexpr int kRows = WAVES > 4 ? R : 4 / WAVES * R;
+  launch("residual_norm", k_residual_norm<T, WAVES, NV, R>,
+         dim3(static_cast<uint32_t>((a.b.rows + kRows - 1) / kRows)),
+         dim3(64 * (WAVES > 4 ? WAVES : 4)), 0, s, a);
+}
+
+template <typename T>
+void choose_forward(const ResidualNorm& a, hipStream_t s) {
+  const bool many = a.b.rows >= 8 * device_cus();
+  const int64_t cols = a.b.cols;
+  if (cols > 16384)
+    launch("residual_norm_long", k_residual_norm_long<T>, dim3(static_cast<uint32_t>(a.b.rows)),
+           dim3(kLong), 0, s, a);
+  else if (cols > 8192) launch_forward<T, 16, 2, 1>(a, s);
+  else if (cols > 4096) launch_forward<T, 4, 4, 1>(a, s);
+  else if (many && cols > 2048) launch_forward<T, 4, 2, 2>(a, s);
+  else if (many && cols > 1024) launch_forward<T, 4, 1, 2>(a, s);
+  else if (cols > 2048) launch_forward<T, 4, 2, 1>(a, s);
+  else if (cols > 1024) launch_forward<T, 4, 1, 1>(a, s);
+  else if (cols > 512) launch_forward<T, 1, 2, 1>(a, s);
+  else launch_forward<T, 1, 1, 1>(a, s);
 }
 
 }  // namespace
 
 hipError_t enqueue_residual_norm(const ResidualNorm& a, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(a.b.rows));
-  if (a.b.type == GARFIELD_F32) launch("residual_norm", k_residual_norm<float>, grid, dim3(kBlock), 0, s, a);
-  else if (a.b.type == GARFIELD_BF16) launch("residual_norm", k_residual_norm<__bf16>, grid, dim3(kBlock), 0, s, a);
-  else launch("residual_norm", k_residual_norm<_Float16>, grid, dim3(kBlock), 0, s, a);
+  if (a.b.type == GARFIELD_F32) choose_forward<float>(a, s);
+  else if (a.b.type == GARFIELD_BF16) choose_forward<__bf16>(a, s);
+  else choose_forward<_Float16>(a, s);
   return hipGetLastError();
 }
 
+// Chunks of equal length, as many as the workgroups that the card holds at once and no more.
 Chunks residual_norm_backward_chunks(const garfield_residual_block& b, int n,
                                      const int64_t* counts) {
-  return make_chunks(n, counts, b.rows < 65536 ? 64 : b.rows / 1024);
+  const int per_cu = b.cols > 2048 ? 1 : b.cols > 1024 ? 2 : b.cols > 512 ? 4 : 8;
+  const int64_t want = static_cast<int64_t>(device_cus()) * per_cu;
+  int64_t per = (b.rows + want - 1) / want;
+  per = per < 2 ? 2 : per;
+  Chunks c = make_chunks(n, counts, per);
+  while (c.chunk0[n] > want && per < b.rows) {
+    per += (per + 31) / 32;
+    c = make_chunks(n, counts, per);
+  }
+  return c;
 }
 
 size_t residual_norm_backward_bytes(const garfield_residual_block& b, const Chunks& c) {
-  return b.rows * sizeof(float2) + static_cast<size_t>(c.chunk0[c.n]) * kSums * b.cols * sizeof(float);
+  const size_t means = b.cols > kBackwardMaxCols ? b.rows * sizeof(float2) : 0;
+  return means + static_cast<size_t>(c.chunk0[c.n]) * kSums * b.cols * sizeof(float);
 }
 
 hipError_t enqueue_residual_norm_backward(const ResidualNormBackward& a, const Chunks& c,
                                           void* workspace, hipStream_t s) {
-  if (a.b.type == GARFIELD_F32) launch_backward<float>(a, c, workspace, s);
-  else if (a.b.type == GARFIELD_BF16) launch_backward<__bf16>(a, c, workspace, s);
-  else launch_backward<_Float16>(a, c, workspace, s);
+  if (a.b.type == GARFIELD_F32) choose_backward<float>(a, c, workspace, s);
+  else if (a.b.type == GARFIELD_BF16) choose_backward<__bf16>(a, c, workspace, s);
+  else choose_backward<_Float16>(a, c, workspace, s);
   return hipGetLastError();
 }
 
