@@ -122,11 +122,35 @@ def test_activations_at_the_edges(name):
     out = gf.linear(p.to(DEV), torch.eye(k, device=DEV), None, name).out
     want = ref.activation(name, p.double())
     want = torch.where(want.isfinite(), want, torch.where(p > 0, p, 0).double())  # p * 0 far below
-    close(out, want, 16 * U * want.abs() + 16 * U * (p.abs() < 30) + 1e-40, "value")
+    # a factor below 2^-126 is no normal fp32 value and becomes 0: |p| 2^-126 where there is one,
+    # which is for |p| < 105
+    small = torch.where(p.abs() < 105, p.abs() * 2.0 ** -126, 0.0).double()
+    close(out, want, 16 * U * want.abs() + 16 * U * (p.abs() < 30) + small + 1e-40, "value")
     k = ref.slope(name, p.double())
     k = torch.where(k.isfinite(), k, (p > 0).double())
     got = gf.activation_backward(torch.ones_like(p).to(DEV), p.to(DEV), name)
     close(got, k, 32 * U * torch.ones_like(k), "slope")
+    nan = torch.full((1, 8), float("nan"), device=DEV)
+    assert bool(gf.linear(nan, torch.eye(8, device=DEV), None, name).out.isnan().all())
+    if name != "relu":  # whose slope is 0 but for p > 0
+        assert bool(gf.activation_backward(torch.ones_like(nan), nan, name).isnan().all())
+
+
+@pytest.mark.parametrize("name", ref.ACTIVATIONS)
+def test_activations_all_along(name):
+    """Every 2^-9 from -16 to 16, in fp32, and gelu's small values relative to themselves."""
+    p = torch.arange(-16 * 512, 16 * 512 + 1, dtype=torch.float32).mul_(2.0 ** -9)[None, :]
+    p = p[:, :p.shape[1] // 64 * 64].reshape(-1, 64)
+    out = gf.linear(p.to(DEV), torch.eye(64, device=DEV), None, name).out
+    want = ref.activation(name, p.double())
+    close(out, want, ref.activation_bound(p.double()), "value")
+    if name != "relu":
+        part = (p > -6) & (p < -0.01)
+        off = ((out.double().cpu() - want) / want)[part].abs().max()
+        assert float(off) < 2.0 ** -12, float(off)
+    k = ref.slope(name, p.double())
+    got = gf.activation_backward(torch.ones_like(p).to(DEV), p.to(DEV), name)
+    close(got, k, ref.slope_bound(p.double()), "slope")
 
 
 @pytest.mark.parametrize("m", [1, 40, 300])
