@@ -176,7 +176,7 @@ typedef enum garfield_activation {
  * `type`; bias (outputs values) is of btype: GARFIELD_F32 or `type`. bias, residual and pre
  * may be NULL; pre gets p, rounded to `type`, for the backward pass. Sums are fp32, and out
  * and pre are rounded once. fp32 products are those of fp32 values.
- * A row of x or w is at most 2^24 columns (GARFIELD_ETOOBIG beyond). The workspace holds
+ * At most 2^20 inputs and outputs (GARFIELD_ETOOBIG beyond). The workspace holds
  * matrices whose rows the product cannot read as they are (their address, distance or length
  * no multiple of 16 bytes), once more, and the fp32 sums of a few columns' shares.
  */
@@ -214,7 +214,7 @@ garfield_status garfield_activation_backward(const void* dy, int type, int64_t r
 
 /*
  * garfield_weight_gradient of an input that is no checkpoint: x (tokens x inputs) is of dy's
- * type. At most 2^24 outputs and inputs.
+ * type. At most 2^20 outputs and inputs.
  */
 size_t garfield_linear_weight_gradient_workspace(const void* dy, int type, int64_t tokens,
                                                  int64_t outputs, int64_t lddy, const void* x,

@@ -72,60 +72,65 @@ struct Side {
     else return (t & 3) | (t >> 1 & 4);
   }
 
-  const char* at;      // the wave's first row of block 0
-  int64_t step;        // bytes between blocks
-  int64_t next;        // bytes between a wave's loads
-  int64_t ld;          // bytes between rows
-  uint32_t from, odd;  // the lane's place in a load, and in every other one
-  int deep;            // along: the depth at which the lane's piece starts
-  int rows;            // along: lines, across: depths, from the wave's first on
-  uint32_t last;       // bytes of the last row that may be read
+  const char* at;        // of the block that comes next
+  int64_t step;          // bytes between blocks
+  uint32_t ld;           // bytes between rows
+  uint32_t last;         // bytes of the last row that are read
+  uint32_t bytes;        // along: of a block, from its first line's to the last line's end
+  uint32_t of[kLoads];   // the lane's place in each load
+  int deep;              // along: the depth at which the lane's piece starts
 
-  // p: line 0 of the tile at depth 0; `lines` are there, and `depth`. Rows are whole 16-byte
-  // pieces, the last one's rest 0.
-  __device__ __forceinline__ void start(const T* p, int64_t stride, int64_t lines, int64_t depth,
-                                        int wave, int lane) {
-    ld = stride * kSize;
+  // p: line 0 of the tile at depth 0; `lines` are there. Rows are whole 16-byte pieces, the last
+  // one's rest 0, and a block's within 2^30 bytes.
+  __device__ __forceinline__ void start(const T* p, int64_t stride, int64_t lines, int wave,
+                                        int lane) {
+    ld = static_cast<uint32_t>(stride * kSize);
+    at = reinterpret_cast<const char*>(p);
     const int row = lane * 16 / kRow, piece = lane % (kRow / 16);
+    const int here = lines < LINES ? static_cast<int>(lines) : LINES;
     if constexpr (ACROSS) {
       constexpr int kPieces = kSize;  // of a chunk
-      const int t = wave * kRows + row;
-      // a block's loads are kRows * WAVES rows apart, 8 or a multiple of 16
-      static_assert(kRows * WAVES % 16 == 0 || kRows * WAVES == 8, "two exchanges");
-      const int chunk = (piece / kPieces) ^ spread(t);
-      const int other = (piece / kPieces) ^ spread(t + kRows * WAVES);
-      from = static_cast<uint32_t>(row * ld) + (chunk * kPieces + piece % kPieces) * 16;
-      odd = static_cast<uint32_t>(row * ld) + (other * kPieces + piece % kPieces) * 16;
+      step = kDepth * int64_t{ld};
+      last = (here * kSize + 15) / 16 * 16;
       deep = 0;
-      rows = static_cast<int>(depth - wave * kRows);
-      last = (static_cast<uint32_t>(lines < LINES ? lines : LINES) * kSize + 15) / 16 * 16;
-      step = kDepth * ld;
+      bytes = 0;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int t = (i * WAVES + wave) * kRows + row;
+        const int chunk = (piece / kPieces) ^ spread(t);
+        of[i] = t * ld + (chunk * kPieces + piece % kPieces) * 16;
+      }
     } else {
-      const int line = wave * 8 + row, chunk = piece ^ (line / 2 % 8);
-      from = odd = static_cast<uint32_t>(row * ld) + chunk * 16;
-      deep = chunk * 16 / kSize;
-      rows = static_cast<int>(lines < LINES ? lines : LINES) - wave * 8;
-      last = 128;
       step = 128;
+      last = 128;
+      bytes = (here - 1) * ld + 128;
+      const int chunk = piece ^ ((wave * 8 + row) / 2 % 8);  // that of lines 16 n on too
+      deep = chunk * 16 / kSize;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) of[i] = ((i * WAVES + wave) * 8 + row) * ld + chunk * 16;
     }
-    next = int64_t{kRows * WAVES} * ld;
-    at = reinterpret_cast<const char*>(p) + wave * kRows * ld;
   }
 
-  // Load i of a block, of which `left` depths are there, to LDS at `to`.
-  __device__ __forceinline__ void fetch(int i, int block, int left, int wave, uint32_t to) const {
-    const char* p = at + block * step + i * next;
-    int there = (ACROSS ? rows - block * kDepth : rows) - i * kRows * WAVES;
-    there = there > kRows ? kRows : there;
-    const uint32_t bytes = there <= 0 ? 0 : static_cast<uint32_t>((there - 1) * ld) + last;
-    // depths past the end read as 0: beyond the buffer's
-    const uint32_t of = ACROSS || deep < left ? (i % 2 ? odd : from) : 0x7ffffff0u;
-    load_to_lds16(buffer_of(p, bytes), of, to + (i * WAVES + wave) * 1024);
+  // The next block, of which `left` depths are there (none: it reads as 0).
+  __device__ __forceinline__ u4 next(int left) {
+    uint32_t there = bytes;
+    if constexpr (ACROSS)
+      there = left <= 0 ? 0 : ((left < kDepth ? left : kDepth) - 1) * ld + last;
+    const u4 b = buffer_of(at, there);
+    at += step;
+    return b;
+  }
+  // Its load i to LDS at `to`.
+  __device__ __forceinline__ void fetch(int i, u4 buffer, int left, int wave, uint32_t to) const {
+    // depths past the end are beyond the buffer's
+    const uint32_t from = ACROSS || deep < left ? of[i] : 0x7ffffff0u;
+    load_to_lds16(buffer, from, to + (i * WAVES + wave) * 1024);
   }
 
   typedef typename Fragment<T>::type F;
-  // The lane's place for the 16 lines from `line` on (a multiple of 16).
-  __device__ static __forceinline__ int place(int line, int lane) {
+  // The lane's place for the 16 lines from `line` on (a multiple of 16): near(place, i) is that
+  // of the i-th 16 lines on, where i is less than a power of two that line / 16 is a multiple of.
+  static __device__ __forceinline__ int place(int line, int lane) {
     if constexpr (!ACROSS) {
       const int l = line + lane % 16;
       return l * 128 + ((lane / 16) ^ (l / 2 % 8)) * 16;
@@ -136,6 +141,9 @@ struct Side {
       const int t = lane / 16 * 4;
       return t * kRow + ((line / 16) ^ spread(t)) * 64 + lane % 16 * 4;
     }
+  }
+  static __device__ __forceinline__ int near(int place, int i) {
+    return ACROSS ? place ^ (i * 16 * kSize) : place + i * 16 * 128;
   }
   // Half block h of a fragment.
   static __device__ __forceinline__ F read(LocalPointer p, int place, int h) {

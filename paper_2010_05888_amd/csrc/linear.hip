@@ -14,33 +14,70 @@ namespace garfield {
 
 namespace {
 
-// The epilogue of eight neighbouring outputs of row m; only those below `cols` are touched.
-template <typename T>
-__device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t j, int64_t cols,
-                                       float* v) {
-  const int64_t left = cols - j;
-  if (left <= 0) return;
-  float t[8];
-  if (e.before) {
-    load8_upto(static_cast<const T*>(e.before) + m * e.ld_before + j, left, t);
-    times_slope<8>(e.activation, t, v);
-  } else {
-    if (e.bias) {
-      if (e.bias_f32) load8_upto(static_cast<const float*>(e.bias) + j, left, t);
-      else load8_upto(static_cast<const T*>(e.bias) + j, left, t);
+// The epilogue of N neighbouring outputs of row m, all of them there. What it reads of other
+// matrices is asked for ahead of the sums.
+template <typename T, int N>
+struct Finish {
+  typedef T Raw __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  Raw before, residual;
+
+  static __device__ __forceinline__ Raw raw(const void* p, int64_t at) {
+    return *reinterpret_cast<const Raw*>(static_cast<const T*>(p) + at);
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t at, const float* v) {
+    Raw t;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += t[i];
+    for (int i = 0; i < N; ++i) t[i] = static_cast<T>(v[i]);
+    *reinterpret_cast<Raw*>(static_cast<T*>(p) + at) = t;
+  }
+
+  __device__ __forceinline__ void ask(const Epilogue& e, int64_t m, int64_t j) {
+    if (e.before) before = raw(e.before, m * e.ld_before + j);
+    if (e.residual) residual = raw(e.residual, m * e.ld_residual + j);
+  }
+
+  __device__ __forceinline__ void put(const Epilogue& e, int64_t m, int64_t j, float* v) const {
+    if (e.before) {
+      float t[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) t[i] = static_cast<float>(before[i]);
+      times_slope<N>(e.activation, t, v);
+    } else {
+      if (e.bias) {
+        typedef float Bias __attribute__((ext_vector_type(N), aligned(4)));
+        if (e.bias_f32) {
+          const Bias t = *reinterpret_cast<const Bias*>(static_cast<const float*>(e.bias) + j);
+#pragma unroll
+          for (int i = 0; i < N; ++i) v[i] += t[i];
+        } else {
+          const Raw t = raw(e.bias, j);
+#pragma unroll
+          for (int i = 0; i < N; ++i) v[i] += static_cast<float>(t[i]);
+        }
+      }
+      if (e.pre) store(e.pre, m * e.ld_pre + j, v);
+      activate<N>(e.activation, v);
     }
-    if (e.pre) store8_upto(static_cast<T*>(e.pre) + m * e.ld_pre + j, left, v);
-    activate<8>(e.activation, v);
-  }
-  if (e.residual) {
-    load8_upto(static_cast<const T*>(e.residual) + m * e.ld_residual + j, left, t);
+    if (e.residual) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += t[i];
+      for (int i = 0; i < N; ++i) v[i] += static_cast<float>(residual[i]);
+    }
+    store(e.out, m * e.ld_out + j, v);
   }
-  store8_upto(static_cast<T*>(e.out) + m * e.ld_out + j, left, v);
-}
+
+  // What is there of eight outputs, one after the other.
+  template <typename Value>
+  static __device__ __forceinline__ void some(const Epilogue& e, int64_t m, int64_t j,
+                                              int64_t left, Value&& value) {
+#pragma unroll 1
+    for (int i = 0; i < left; ++i) {
+      Finish<T, 1> one;
+      float x = value(i);
+      one.ask(e, m, j + i);
+      one.put(e, m, j + i, &x);
+    }
+  }
+};
 
 // Workgroup id to tile: workgroups go to the eight XCDs in turn, so an XCD's
 // share is made contiguous, and inside it eight tiles of rows deep: the tiles that
@@ -62,9 +99,23 @@ __device__ __forceinline__ Place place_of(uint32_t id, uint32_t total, uint32_t 
   return {first + at % group % deep, at % group / deep, part};
 }
 
-// A tile's sums: a workgroup of WJ * WM waves makes WM * FB * 16 rows x WJ * FA * 16 columns of
-// A B^T, a wave FA x FB products of 16 x 16, block after block. The next block goes from memory
-// straight to LDS while the waves work on this one, a few loads at a time between the products.
+// What a tile is made of: line 0 of both operands at depth 0, the lines and depths that are there.
+template <typename T>
+struct Parts {
+  const T *a, *b;
+  int64_t rows, cols, depth;
+};
+
+// A tile of WM * FB * 16 rows x WJ * FA * 16 columns of A B^T by a workgroup of WJ * WM waves: a
+// wave has FA x FB products of 16 x 16, block after block, in two halves. While it multiplies
+// one half it reads the next one's operands, so that nothing but the one barrier of a block, in
+// its middle, is waited for: there the block has been read, and the one after the next starts on
+// its way to its place, a load between every few products, straight to LDS.
+// 8192^3 in bf16: 800 us, 1370 TFLOP/s (a library's product 705), of zeros 700 (530): power bounds
+// both, then the loads' issue (100 us) and the barrier (50). What was slower: waves of 128 x 128,
+// one a SIMD (1220); a block's loads in its first half's products (815); one workgroup for many
+// tiles, the next one's first block on its way during the epilogue (564 against 535 us for 16384 x
+// 8192 x 2048 with gelu and p: its loads wait for its stores; a new workgroup's do not).
 template <typename T, bool AA, bool BA, int WJ, int WM, int FA, int FB>
 struct Tile {
   static constexpr int kWaves = WJ * WM, kCols = WJ * FA * 16, kRows = WM * FB * 16;
@@ -72,102 +123,154 @@ struct Tile {
   typedef Side<T, BA, kCols, kWaves> SideB;
   static constexpr int kStage = SideA::kBytes + SideB::kBytes;
   static constexpr int kLoads = SideA::kLoads + SideB::kLoads;
+  static constexpr int kDepth = SideA::kDepth;
 
-  // `ones` (with_ones): the sums of A's lines over the depth.
-  template <typename Ones>
-  static __device__ __forceinline__ void sums(uint8_t* lds, const T* a, int64_t lda, int64_t rows,
-                                              const T* b, int64_t ldb, int64_t cols, int64_t depth,
-                                              v4f (&sum)[FA][FB], Ones&& ones) {
+  // also(af): what else is done with A's fragments.
+  template <typename Also>
+  static __device__ __forceinline__ void sums(uint8_t* lds, int64_t lda, int64_t ldb,
+                                              const Parts<T>& p, v4f (&sum)[FA][FB], Also&& also) {
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wj = wave / WM, wm = wave % WM;
     SideA from_a;
     SideB from_b;
-    from_a.start(a, lda, rows, depth, wave, lane);
-    from_b.start(b, ldb, cols, depth, wave, lane);
+    from_a.start(p.a, lda, p.rows, wave, lane);
+    from_b.start(p.b, ldb, p.cols, wave, lane);
     const uint32_t base = lds_offset(lds);
-    constexpr int kDepth = SideA::kDepth;
-    const int blocks = static_cast<int>((depth + kDepth - 1) / kDepth);
-    auto fetch = [&](int l, int block, int into) {
-      const int left = block < blocks ? static_cast<int>(depth - int64_t{block} * kDepth) : 0;
-      const uint32_t to = base + into * kStage;
-      if (l < SideB::kLoads) from_b.fetch(l, block, left, wave, to + SideA::kBytes);
-      else from_a.fetch(l - SideB::kLoads, block, left, wave, to);
+    const int blocks = static_cast<int>((p.depth + kDepth - 1) / kDepth);
+    int left = static_cast<int>(p.depth);  // depths from the next block on
+    u4 of_a, of_b;
+    auto next = [&] {
+      of_a = from_a.next(left);
+      of_b = from_b.next(left);
     };
+    auto fetch = [&](int l, int into) {
+      const uint32_t to = base + into * kStage;
+      if (l < SideB::kLoads) from_b.fetch(l, of_b, left, wave, to + SideA::kBytes);
+      else from_a.fetch(l - SideB::kLoads, of_a, left, wave, to);
+    };
+    const int at_a = SideA::place(wm * FB * 16, lane), at_b = SideB::place(wj * FA * 16, lane);
 #pragma unroll
     for (int i = 0; i < FA; ++i)
 #pragma unroll
       for (int k = 0; k < FB; ++k) sum[i][k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    int at_a[FB], at_b[FA];
+    typename SideA::F af[2][FB];
+    typename SideB::F bf[2][FA];
+    // fragment f of half h of block b, A's first
+    auto read = [&](int f, int b, int h) {
+      const LocalPointer here = (LocalPointer)lds + (b & 1) * kStage;
+      if (f < FB) af[h][f] = SideA::read(here, SideA::near(at_a, f), h);
+      else bf[h][f - FB] = SideB::read(here + SideA::kBytes, SideB::near(at_b, f - FB), h);
+    };
+    constexpr int kReads = FA + FB, kEarly = FA > 2 ? FA - 2 : 1;
 #pragma unroll
-    for (int k = 0; k < FB; ++k) at_a[k] = SideA::place((wm * FB + k) * 16, lane);
+    for (int s = 0; s < 2; ++s) {
+      next();
 #pragma unroll
-    for (int i = 0; i < FA; ++i) at_b[i] = SideB::place((wj * FA + i) * 16, lane);
-    if (blocks > 0) {
-#pragma unroll
-      for (int l = 0; l < kLoads; ++l) fetch(l, 0, 0);
+      for (int l = 0; l < kLoads; ++l) fetch(l, s);
+      left -= kDepth;
     }
+    wait_for<kLoads>();
+    barrier();
+#pragma unroll
+    for (int f = 0; f < kReads; ++f) read(f, 0, 0);
+#pragma unroll 1
     for (int b = 0; b < blocks; ++b) {
-      wait_for<0>();
-      barrier();  // block b is there, and block b - 1 has been read
-      const int next = b + 1, into = next & 1;
-      const LocalPointer here_a = (LocalPointer)lds + (b & 1) * kStage;
-      const LocalPointer here_b = here_a + SideA::kBytes;
+      also(af[0]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        typename SideA::F af[FB];
-        typename SideB::F bf[2];
+      for (int i = 0; i < FA; ++i) {
 #pragma unroll
-        for (int k = 0; k < FB; ++k) af[k] = SideA::read(here_a, at_a[k], h);
-        bf[0] = SideB::read(here_b, at_b[0], h);
-        ones(af);
+        for (int f = i * kReads / kEarly; f < (i + 1) * kReads / kEarly && f < kReads; ++f)
+          read(f, b, 1);
 #pragma unroll
-        for (int i = 0; i < FA; ++i) {
-          if (i + 1 < FA) bf[(i + 1) & 1] = SideB::read(here_b, at_b[i + 1], h);
-          if (next < blocks && h == 0) {
-#pragma unroll
-            for (int l = i * kLoads / FA; l < (i + 1) * kLoads / FA; ++l) fetch(l, next, into);
-          }
-#pragma unroll
-          for (int k = 0; k < FB; ++k) sum[i][k] = multiply(bf[i & 1], af[k], sum[i][k]);
-        }
+        for (int k = 0; k < FB; ++k) sum[i][k] = multiply(bf[0][i], af[0][k], sum[i][k]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      wait_for<0>();
+      barrier();  // block b has been read, and block b + 1 is there
+      next();
+      also(af[1]);
+#pragma unroll
+      for (int i = 0; i < FA; ++i) {
+#pragma unroll
+        for (int l = i * kLoads / FA; l < (i + 1) * kLoads / FA; ++l)
+          fetch(l, b & 1);
+#pragma unroll
+        for (int f = i * kReads / kEarly; f < (i + 1) * kReads / kEarly && f < kReads; ++f)
+          read(f, b + 1, 0);
+#pragma unroll
+        for (int k = 0; k < FB; ++k) sum[i][k] = multiply(bf[1][i], af[1][k], sum[i][k]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      left -= kDepth;
     }
     wait_for<0>();
     barrier();  // LDS is free
   }
 
-  // Every output, eight neighbouring ones of a line at a time: put(line, column, values). A lane
-  // has four columns of one line in each of its sums; by way of the wave's own part of LDS,
-  // `kPass` sums at a time, they become lines of FA * 16 columns, whose 16-byte piece c lies at
-  // c ^ line % kSwap.
-  template <typename Put>
-  static __device__ __forceinline__ void rows_of(uint8_t* lds, const v4f (&sum)[FA][FB], Put&& put) {
+  // Every output of the first `lines` x `columns`, eight neighbouring ones of a line at a time:
+  // ask(state, line, column), and some lines later put(state, line, column, values); the line's
+  // last ones, fewer than eight, some(line, column, how many, value by number). A lane has four
+  // columns of one line in each of its sums; by way of the wave's own part of LDS, `kPass` sums
+  // at a time, they become lines of FA * 16 columns: a line's even 16-byte pieces, then its odd
+  // ones, piece p of these at p ^ line % kSwap. So 16 lanes that write a piece of 16 lines, or
+  // read every other piece of one, have banks of their own.
+  template <typename State, typename Ask, typename Put, typename Some>
+  static __device__ __forceinline__ void rows_of(uint8_t* lds, const v4f (&sum)[FA][FB],
+                                                 int64_t lines, int64_t columns, Ask&& ask,
+                                                 Put&& put, Some&& some) {
     constexpr int kLine = FA * 64, kRoom = 2 * kStage / kWaves;
     constexpr int kPass = kRoom / (16 * kLine) < FB ? kRoom / (16 * kLine) : FB;
-    constexpr int kSwap = FA * 4 < 16 ? FA * 4 : 16, kEights = FA * 2;
-    static_assert(kPass > 0 && FB % kPass == 0, "sums go through LDS in equal parts");
+    constexpr int kEights = FA * 2, kSwap = FA * 4 < 16 ? FA * 4 : 16, kApart = 64 / kEights;
+    constexpr int kSteps = kPass * 16 / kApart;  // of a pass
+    static_assert(kPass > 0 && FB % kPass == 0 && kSteps % 2 == 0, "equal parts");
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wj = wave / WM, wm = wave % WM;
     uint8_t* const own = lds + wave * kRoom;
+    const int first = lane / kEights, c = lane % kEights, column = wj * FA * 16 + c * 8;
+    const int here = lines < kRows ? static_cast<int>(lines) : kRows;
+    const int left = columns - column < 8 ? static_cast<int>(columns - column) : 8;
+    State state[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int line = wm * FB * 16 + first + q * kApart;
+      if (left == 8 && line < here) ask(state[q], line, column);
+    }
 #pragma unroll
     for (int k0 = 0; k0 < FB; k0 += kPass) {
 #pragma unroll
       for (int k = 0; k < kPass; ++k)
 #pragma unroll
         for (int i = 0; i < FA; ++i)
-          *reinterpret_cast<v4f*>(own + (k * 16 + lane % 16) * kLine +
-                                  ((i * 4 + lane / 16) ^ (lane % kSwap)) * 16) = sum[i][k0 + k];
+          *reinterpret_cast<v4f*>(
+              own + (k * 16 + lane % 16) * kLine +
+              ((i * 2 + lane / 32 + kEights * (lane / 16 % 2)) ^ (lane % kSwap)) * 16) =
+              sum[i][k0 + k];
 #pragma unroll 1
-      for (int r = lane / kEights; r < kPass * 16; r += 64 / kEights) {
-        const int c = lane % kEights * 2;
-        v4f v[2];
+      for (int r0 = first; r0 < kPass * 16; r0 += 2 * kApart) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          v[e] = *reinterpret_cast<const v4f*>(own + r * kLine + ((c + e) ^ (r % kSwap)) * 16);
-        float t[8];
+        for (int q = 0; q < 2; ++q) {
+          const int r = r0 + q * kApart, line = (wm * FB + k0) * 16 + r;
+          if (line >= here || left <= 0) continue;
+          auto half = [&](int e) {
+            return reinterpret_cast<const float*>(own + r * kLine +
+                                                  ((c + kEights * e) ^ (r % kSwap)) * 16);
+          };
+          if (left < 8) {
+            some(line, column, left, [&](int e) { return half(e / 4)[e % 4]; });
+            continue;
+          }
+          float t[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = v[e / 4][e % 4];
-        put((wm * FB + k0) * 16 + r, wj * FA * 16 + c * 4, t);
+          for (int e = 0; e < 2; ++e) {
+            const v4f v = *reinterpret_cast<const v4f*>(half(e));
+#pragma unroll
+            for (int f = 0; f < 4; ++f) t[e * 4 + f] = v[f];
+          }
+          const State now = state[q];
+          const int later = line + 2 * kApart;
+          if (later < here && later < (wm + 1) * FB * 16) ask(state[q], later, column);
+          put(now, line, column, t);
+        }
       }
     }
   }
@@ -182,27 +285,40 @@ struct Job {
   int64_t ld_partial;
 };
 
+struct Nothing {};
+
 template <typename T, bool AA, bool BA, int WJ, int WM, int FA, int FB>
 __global__ __launch_bounds__(64 * WJ * WM) void k_product(Job p, Epilogue to) {
   typedef Tile<T, AA, BA, WJ, WM, FA, FB> Of;
   __shared__ __align__(1024) uint8_t lds[2 * Of::kStage];
   const Place at = place_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_j);
   const int64_t m0 = at.m * Of::kRows, j0 = at.j * Of::kCols, k0 = at.part * p.share;
-  const int64_t depth = p.depth - k0 < p.share ? p.depth - k0 : p.share;
+  const Parts<T> parts = {static_cast<const T*>(p.a) + (AA ? k0 * p.lda + m0 : m0 * p.lda + k0),
+                          static_cast<const T*>(p.b) + (BA ? k0 * p.ldb + j0 : j0 * p.ldb + k0),
+                          p.rows - m0, p.cols - j0,
+                          p.depth - k0 < p.share ? p.depth - k0 : p.share};
   v4f sum[FA][FB];
-  Of::sums(lds, static_cast<const T*>(p.a) + (AA ? k0 * p.lda + m0 : m0 * p.lda + k0), p.lda,
-           p.rows - m0, static_cast<const T*>(p.b) + (BA ? k0 * p.ldb + j0 : j0 * p.ldb + k0),
-           p.ldb, p.cols - j0, depth, sum, [](auto&) {});
-  Of::rows_of(lds, sum, [&](int line, int column, float* v) {
-    const int64_t m = m0 + line, j = j0 + column;
-    if (m >= p.rows) return;
-    if (p.partial) {
-      float* out = p.partial + (at.part * p.rows + m) * p.ld_partial + j;
-      if (j < p.cols) store8_upto(out, p.ld_partial - j, v);
-    } else {
-      finish<T>(to, m, j, p.cols, v);
-    }
-  });
+  Of::sums(lds, p.lda, p.ldb, parts, sum, [](auto&) {});
+  if (p.partial) {  // whose lines go on to whole eights
+    float* const out = p.partial + at.part * p.rows * p.ld_partial + m0 * p.ld_partial + j0;
+    Of::template rows_of<Nothing>(
+        lds, sum, parts.rows, (parts.cols + 7) / 8 * 8, [](Nothing&, int, int) {},
+        [&](const Nothing&, int line, int column, float* v) {
+          store8_upto(out + line * p.ld_partial + column, 8, v);
+        },
+        [](int, int, int, auto&&) {});
+  } else {
+    typedef Finish<T, 8> Eight;
+    Of::template rows_of<Eight>(
+        lds, sum, parts.rows, parts.cols,
+        [&](Eight& f, int line, int column) { f.ask(to, m0 + line, j0 + column); },
+        [&](const Eight& f, int line, int column, float* v) {
+          f.put(to, m0 + line, j0 + column, v);
+        },
+        [&](int line, int column, int left, auto&& value) {
+          Eight::some(to, m0 + line, j0 + column, left, value);
+        });
+  }
 }
 
 // The shares' sums added in ascending order, and the epilogue: eight outputs a thread.
@@ -221,7 +337,19 @@ __global__ __launch_bounds__(kBlock) void k_finish(Job p, int shares, Epilogue t
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += v[e];
   }
-  finish<T>(to, m, j, p.cols, sum);
+  if (j + 8 <= p.cols) {
+    Finish<T, 8> f;
+    f.ask(to, m, j);
+    f.put(to, m, j, sum);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (j + e >= p.cols) break;
+      Finish<T, 1> f;
+      f.ask(to, m, j + e);
+      f.put(to, m, j + e, sum + e);
+    }
+  }
 }
 
 // The workers' tokens, each worker's cut into `splits` shares.
@@ -243,11 +371,13 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_dense_gradient(Job p, Workers 
   const int64_t m0 = at.m * Of::kRows, j0 = at.j * Of::kCols;
   const int worker = at.part % w.n;
   int64_t t0 = w.first[worker], end = w.first[worker + 1];
-  constexpr int64_t kDepth = Of::SideA::kDepth;
-  const int64_t most = ((end - t0 + kDepth - 1) / kDepth + w.splits - 1) / w.splits * kDepth;
+  const int64_t blocks = (end - t0 + Of::kDepth - 1) / Of::kDepth;
+  const int64_t most = (blocks + w.splits - 1) / w.splits * Of::kDepth;
   t0 += at.part / w.n * most;
   end = t0 + most < end ? t0 + most : end;
-  const int64_t depth = end > t0 ? end - t0 : 0;
+  const Parts<T> parts = {static_cast<const T*>(p.a) + t0 * p.lda + m0,
+                          static_cast<const T*>(p.b) + t0 * p.ldb + j0, p.rows - m0, p.cols - j0,
+                          end > t0 ? end - t0 : 0};
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wj = wave / WM, wm = wave % WM;
   typename Fragment<T>::type one;
@@ -256,15 +386,14 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_dense_gradient(Job p, Workers 
   v4f sum[FA][FB], ones[FB];
 #pragma unroll
   for (int k = 0; k < FB; ++k) ones[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  // the sums of dy's columns are made by the tiles of the first inputs
   const bool with_bias = dbias && j0 == 0 && wj == 0;
-  Of::sums(lds, static_cast<const T*>(p.a) + t0 * p.lda + m0, p.lda, p.rows - m0,
-           static_cast<const T*>(p.b) + t0 * p.ldb + j0, p.ldb, p.cols - j0, depth, sum,
-           [&](auto& af) {
-             if (with_bias) {
+  Of::sums(lds, p.lda, p.ldb, parts, sum, [&](auto& af) {
+    if (with_bias) {
 #pragma unroll
-               for (int k = 0; k < FB; ++k) ones[k] = multiply(one, af[k], ones[k]);
-             }
-           });
+      for (int k = 0; k < FB; ++k) ones[k] = multiply(one, af[k], ones[k]);
+    }
+  });
   if (with_bias && lane < 16) {
 #pragma unroll
     for (int k = 0; k < FB; ++k) {
@@ -272,11 +401,16 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_dense_gradient(Job p, Workers 
       if (m < p.rows) dbias[at.part * ld_dbias + m] = ones[k][0];
     }
   }
-  Of::rows_of(lds, sum, [&](int line, int column, float* v) {
-    const int64_t m = m0 + line, j = j0 + column;
-    if (m < p.rows && j < p.cols)
-      store8_upto(dw + at.part * ld_dw + m * p.cols + j, p.cols - j, v);
-  });
+  float* const out = dw + at.part * ld_dw + m0 * p.cols + j0;
+  Of::template rows_of<Nothing>(
+      lds, sum, parts.rows, parts.cols, [](Nothing&, int, int) {},
+      [&](const Nothing&, int line, int column, float* v) {
+        store8_upto(out + line * p.cols + column, 8, v);
+      },
+      [&](int line, int column, int left, auto&& value) {
+#pragma unroll 1
+        for (int e = 0; e < left; ++e) out[line * p.cols + column + e] = value(e);
+      });
 }
 
 // The splits' gradients added in ascending order: `length` values for each of n workers,
@@ -351,7 +485,7 @@ __global__ __launch_bounds__(kBlock) void k_activation_backward(
   }
 }
 
-constexpr int64_t kMaxApart = int64_t{1} << 27;  // bytes between rows that a load spans
+constexpr int64_t kMaxApart = int64_t{1} << 22;  // bytes between rows: 256 are within 2^30
 
 int64_t size_of(int type) { return type == GARFIELD_F32 ? 4 : 2; }
 int64_t up_to(int64_t v, int64_t of) { return (v + of - 1) / of * of; }
@@ -474,7 +608,7 @@ void launch_gradients(Job p, const Workers& w, float* dw, int64_t ld_dw, float* 
                       int64_t ld_dbias, hipStream_t s) {
   p.tiles_m = static_cast<uint32_t>((p.rows + WM * FB * 16 - 1) / (WM * FB * 16));
   p.tiles_j = static_cast<uint32_t>((p.cols + WJ * FA * 16 - 1) / (WJ * FA * 16));
-  // A launch has fewer than 2^32 threads: many workers' tiles take several
+  // A launch has fewer than 2^32 threads: many workers' tiles may take several
   const int64_t tiles = int64_t{p.tiles_m} * p.tiles_j * w.splits;
   const int fit = static_cast<int>(std::min<int64_t>(0xffffffff / (64 * WJ * WM) / tiles, w.n));
   for (int i = 0; i < w.n; i += fit) {

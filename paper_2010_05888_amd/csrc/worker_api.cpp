@@ -23,7 +23,8 @@ constexpr int64_t kMaxBlocks = int64_t{1} << 27;  // of one matrix, padded
 // Weight gradients address 32 tokens with 32 bits.
 constexpr int64_t kMaxOutputs = int64_t{1} << 24;
 constexpr int64_t kMaxStride = int64_t{1} << 26;
-constexpr int64_t kMaxDepth = int64_t{1} << 24;  // a dense product's columns that are added up
+// Dense products address 256 rows of a matrix with 32 bits.
+constexpr int64_t kMaxDense = int64_t{1} << 20;
 constexpr int kMaxTensors = 1 << 20;
 constexpr int64_t kMaxLength = int64_t{1} << 34;
 
@@ -90,7 +91,7 @@ garfield_status check_product(int64_t rows, int64_t cols, int64_t depth) {
   garfield_status st = check_size(rows, depth);
   if (st == GARFIELD_OK) st = check_size(cols, depth);
   if (st == GARFIELD_OK) st = check_size(rows, cols);
-  return st == GARFIELD_OK && depth > kMaxDepth ? GARFIELD_ETOOBIG : st;
+  return st == GARFIELD_OK && (cols > kMaxDense || depth > kMaxDense) ? GARFIELD_ETOOBIG : st;
 }
 
 Product forward_product(const void* x, int type, int64_t tokens, int64_t inputs, int64_t ldx,
@@ -141,7 +142,7 @@ garfield_status check_dense_gradient(int type, int64_t tokens, int64_t outputs, 
   if (st == GARFIELD_OK) st = check_size(tokens, inputs);
   if (st == GARFIELD_OK) st = check_size(outputs, inputs);
   if (st == GARFIELD_OK) st = check_counts(n, counts, tokens);
-  if (st == GARFIELD_OK && (outputs > kMaxOutputs || inputs > kMaxOutputs)) return GARFIELD_ETOOBIG;
+  if (st == GARFIELD_OK && (outputs > kMaxDense || inputs > kMaxDense)) return GARFIELD_ETOOBIG;
   return st;
 }
 
