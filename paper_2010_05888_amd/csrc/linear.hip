@@ -222,16 +222,17 @@ struct Tile {
     constexpr int kPass = kRoom / (16 * kLine) < FB ? kRoom / (16 * kLine) : FB;
     constexpr int kEights = FA * 2, kSwap = FA * 4 < 16 ? FA * 4 : 16, kApart = 64 / kEights;
     constexpr int kSteps = kPass * 16 / kApart;  // of a pass
-    static_assert(kPass > 0 && FB % kPass == 0 && kSteps % 2 == 0, "equal parts");
+    constexpr int kAsked = kSteps % 2 == 0 ? 2 : 1;
+    static_assert(kPass > 0 && FB % kPass == 0, "equal parts");
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wj = wave / WM, wm = wave % WM;
     uint8_t* const own = lds + wave * kRoom;
     const int first = lane / kEights, c = lane % kEights, column = wj * FA * 16 + c * 8;
     const int here = lines < kRows ? static_cast<int>(lines) : kRows;
     const int left = columns - column < 8 ? static_cast<int>(columns - column) : 8;
-    State state[2];
+    State state[kAsked];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < kAsked; ++q) {
       const int line = wm * FB * 16 + first + q * kApart;
       if (left == 8 && line < here) ask(state[q], line, column);
     }
@@ -246,9 +247,9 @@ struct Tile {
               ((i * 2 + lane / 32 + kEights * (lane / 16 % 2)) ^ (lane % kSwap)) * 16) =
               sum[i][k0 + k];
 #pragma unroll 1
-      for (int r0 = first; r0 < kPass * 16; r0 += 2 * kApart) {
+      for (int r0 = first; r0 < kPass * 16; r0 += kAsked * kApart) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < kAsked; ++q) {
           const int r = r0 + q * kApart, line = (wm * FB + k0) * 16 + r;
           if (line >= here || left <= 0) continue;
           auto half = [&](int e) {
@@ -267,7 +268,7 @@ struct Tile {
             for (int f = 0; f < 4; ++f) t[e * 4 + f] = v[f];
           }
           const State now = state[q];
-          const int later = line + 2 * kApart;
+          const int later = line + kAsked * kApart;
           if (later < here && later < (wm + 1) * FB * 16) ask(state[q], later, column);
           put(now, line, column, t);
         }
@@ -318,6 +319,91 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_product(Job p, Epilogue to) {
         [&](int line, int column, int left, auto&& value) {
           Eight::some(to, m0 + line, j0 + column, left, value);
         });
+  }
+}
+
+// Few rows (up to 16), B along: the time is B's bytes, or latency where they are few (one
+// token, 4096 x 4096 in bf16: 7.5 us, 4.5 TB/s, against 8.7 + 4.8 us in tiles with shares). A
+// workgroup takes 16 columns, its waves every WAVES-th block each, fragments straight from memory
+// and several blocks at a time; the waves' sums meet in LDS, added in one order. Any address and
+// distance of rows is taken.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_product_few(Job p, Epilogue to) {
+  typedef typename Fragment<T>::type F;
+  typedef T Loose __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+  constexpr int kAtOnce = 4, kDepth = 128 / sizeof(T), kPiece = 16 / sizeof(T);
+  __shared__ v4f sums[WAVES][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t j0 = static_cast<int64_t>(blockIdx.x) * 16;
+  const int64_t line = j0 + lane % 16 < p.cols ? j0 + lane % 16 : p.cols - 1;
+  const T* const from_b = static_cast<const T*>(p.b) + line * p.ldb;
+  const int64_t m = lane % 16 < p.rows ? lane % 16 : p.rows - 1;
+  const T* const from_a = static_cast<const T*>(p.a) + m * p.lda;
+  v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t c0 = lane / 16 * kPiece;
+  auto whole_piece = [&](const T* q, int64_t c) {
+    const Loose t = *reinterpret_cast<const Loose*>(q + c);
+    F v;
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e) v[e] = t[e];
+    return v;
+  };
+  auto some_piece = [&](const T* q, int64_t c) {  // zeros past the depth
+    F v;
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e) v[e] = c + e < p.depth ? q[c + e] : static_cast<T>(0.0f);
+    return v;
+  };
+  const int blocks = static_cast<int>((p.depth + kDepth - 1) / kDepth);
+  const int whole_blocks = static_cast<int>(p.depth / kDepth);
+  int b0 = wave;
+  for (; b0 + (kAtOnce - 1) * WAVES < whole_blocks; b0 += WAVES * kAtOnce) {
+    F bf[kAtOnce][2], af[kAtOnce][2];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t c = (b0 + u * WAVES) * int64_t{kDepth} + h * 4 * kPiece + c0;
+        bf[u][h] = whole_piece(from_b, c);
+        af[u][h] = whole_piece(from_a, c);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sum = multiply(bf[u][h], af[u][h], sum);
+  }
+  for (; b0 < blocks; b0 += WAVES) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t c = b0 * int64_t{kDepth} + h * 4 * kPiece + c0;
+      const bool there = b0 < whole_blocks;
+      sum = multiply(there ? whole_piece(from_b, c) : some_piece(from_b, c),
+                     there ? whole_piece(from_a, c) : some_piece(from_a, c), sum);
+    }
+  }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  const int64_t j = j0 + lane / 16 * 4;
+  if (wave > 0 || lane % 16 >= p.rows) return;
+  v4f all = sums[0][lane];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) all += sums[i][lane];
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = all[e];
+  if (j + 4 <= p.cols) {
+    Finish<T, 4> f;
+    f.ask(to, m, j);
+    f.put(to, m, j, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e >= p.cols) break;
+      Finish<T, 1> f;
+      f.ask(to, m, j + e);
+      f.put(to, m, j + e, v + e);
+    }
   }
 }
 
@@ -433,27 +519,34 @@ __global__ __launch_bounds__(kBlock) void k_sum_shares(const float* __restrict__
   store8_upto(out + blockIdx.y * ld + i, length - i, sum);
 }
 
-// A matrix once more, with rows of whole 16-byte pieces (the last one's rest 0).
+// Matrices once more, with rows of whole 16-byte pieces (the last one's rest 0): the first
+// `groups` workgroups the first one, the others the second.
+struct Packed {
+  const void* from;
+  int64_t ld, rows, cols;
+  void* to;
+  int64_t ld_to;
+};
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_pack_rows(const T* __restrict__ x, int64_t ld,
-                                                      int64_t rows, int64_t cols,
-                                                      T* __restrict__ out, int64_t ld_out) {
+__global__ __launch_bounds__(kBlock) void k_pack_rows(Packed first, Packed second, uint32_t groups) {
   constexpr int kPiece = 16 / sizeof(T);
   typedef T Piece __attribute__((ext_vector_type(kPiece)));
   typedef T Loose __attribute__((ext_vector_type(kPiece), aligned(sizeof(T))));
-  const int64_t pieces = ld_out / kPiece;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < rows * pieces;
-       i += static_cast<int64_t>(gridDim.x) * kBlock) {
+  const bool later = blockIdx.x >= groups;
+  const Packed m = later ? second : first;
+  const int64_t pieces = m.ld_to / kPiece, group = later ? blockIdx.x - groups : blockIdx.x;
+  const int64_t all = later ? gridDim.x - groups : groups;
+  for (int64_t i = group * kBlock + threadIdx.x; i < m.rows * pieces; i += all * kBlock) {
     const int64_t r = i / pieces, c = i % pieces * kPiece;
-    const T* p = x + r * ld + c;
+    const T* p = static_cast<const T*>(m.from) + r * m.ld + c;
     Piece v;
-    if (c + kPiece <= cols) {
+    if (c + kPiece <= m.cols) {
       v = *reinterpret_cast<const Loose*>(p);
     } else {
 #pragma unroll
-      for (int e = 0; e < kPiece; ++e) v[e] = c + e < cols ? p[e] : static_cast<T>(0.0f);
+      for (int e = 0; e < kPiece; ++e) v[e] = c + e < m.cols ? p[e] : static_cast<T>(0.0f);
     }
-    *reinterpret_cast<Piece*>(out + i * kPiece) = v;
+    *reinterpret_cast<Piece*>(static_cast<T*>(m.to) + i * kPiece) = v;
   }
 }
 
@@ -500,49 +593,70 @@ size_t packed_bytes(int64_t rows, int64_t cols, int64_t size) {
   return static_cast<size_t>(up_to(rows * up_to(cols * size, 16), 256));
 }
 
-// The matrix as the product reads it; `rest`: the workspace from here on.
+// The matrix as the product reads it: as it is, or its place in the workspace (`rest`: from here
+// on), to be packed there.
 template <typename T>
-const T* whole(const void* p, int64_t* ld, int64_t rows, int64_t cols, char** rest, hipStream_t s) {
-  constexpr int64_t kPiece = 16 / sizeof(T);
+Packed whole(const void* p, int64_t* ld, int64_t rows, int64_t cols, char** rest) {
+  Packed m = {p, *ld, rows, cols, nullptr, 0};
   if (is_whole(p, *ld, rows, cols, sizeof(T))) {
     if (rows < 2) *ld = cols;
-    return static_cast<const T*>(p);
+  } else {
+    m.to = *rest;
+    *ld = m.ld_to = up_to(cols, 16 / sizeof(T));
+    *rest += packed_bytes(rows, cols, sizeof(T));
   }
-  T* out = reinterpret_cast<T*>(*rest);
-  const int64_t ld_out = up_to(cols, kPiece);
-  const int64_t groups = (rows * (ld_out / kPiece) + kBlock - 1) / kBlock, most = int64_t{1} << 23;
-  if (groups > 0)
-    launch("pack_rows", k_pack_rows<T>, dim3(static_cast<uint32_t>(groups < most ? groups : most)),
-           dim3(kBlock), 0, s, static_cast<const T*>(p), *ld, rows, cols, out, ld_out);
-  *rest += packed_bytes(rows, cols, sizeof(T));
-  *ld = ld_out;
-  return out;
+  return m;
+}
+
+// Packs what has to be, and gives where both are then.
+template <typename T>
+void pack(const Packed& a, const Packed& b, const void** at_a, const void** at_b, hipStream_t s) {
+  auto groups = [](const Packed& m) {
+    const int64_t g = m.to ? (m.rows * (m.ld_to * sizeof(T) / 16) + kBlock - 1) / kBlock : 0;
+    return static_cast<uint32_t>(std::min(g, int64_t{1} << 22));
+  };
+  const uint32_t first = groups(a), second = groups(b);
+  if (first + second > 0)
+    launch("pack_rows", k_pack_rows<T>, dim3(first + second), dim3(kBlock), 0, s, a, b, first);
+  *at_a = a.to ? a.to : a.from;
+  *at_b = b.to ? b.to : b.from;
 }
 
 int64_t tiles_of(int64_t rows, int64_t cols, int size) {
   return ((rows + size - 1) / size) * ((cols + size - 1) / size);
 }
 
-// Tiles of 64, 128 or 256 lines, and into how many shares their depth is cut.
+// Tiles of 64, 128 or 256 lines (32: of 32 rows x 64 columns), and into how many shares their
+// depth is cut.
 struct Plan {
   int size, shares;
   int64_t share;  // depths
 };
 
+// The largest tile of which there are 192 (of 256 CUs): in bf16 3500 x 3500 x 2000, 196 tiles of
+// 256 x 256, takes 66 us and 76 in tiles of 128; 2048 x 4096 x 4096, 128 of 256, takes 64 in tiles
+// of 128 and 84 in those; 1000 x 2000 x 3000, 512 of 64, 30 in tiles of 64 and 43 in 128. Few
+// tiles of much depth are cut into shares of ten blocks or more, up to two for a CU: 128 x 512 x
+// 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole. An fp32
+// tile takes its products' time, whatever its neighbours: between one and four for a CU, rows
+// are halved where that shares them out better (777 x 1500 x 1000, 312 tiles or 600: 40 us and 30).
 Plan plan_product(int64_t rows, int64_t cols, int64_t depth, int64_t size) {
   const int64_t block = 128 / size, blocks = (depth + block - 1) / block;
   Plan p = {64, 1, (blocks > 0 ? blocks : 1) * block};
-  if (tiles_of(rows, cols, 256) >= 192) {
+  const int64_t cus = device_cus(), tiles = tiles_of(rows, cols, 64);
+  if (tiles_of(rows, cols, 256) >= cus * 3 / 4) {
     p.size = 256;
-  } else if (tiles_of(rows, cols, 128) >= 192) {
+  } else if (tiles_of(rows, cols, 128) >= cus * 3 / 4) {
     p.size = 128;
-  } else if (rows > 0 && cols > 0) {
-    const int64_t tiles = tiles_of(rows, cols, 64), most = 3 * int64_t{device_cus()};
-    const int64_t want = std::min(most / tiles, blocks / 4);
+  } else if (tiles > 0) {
+    const int64_t want = std::min(2 * cus / tiles, blocks / 10);
     if (want >= 2) {
       const int64_t per = (blocks + want - 1) / want;
       p.share = per * block;
       p.shares = static_cast<int>((blocks + per - 1) / per);
+    } else if (size == 4 && tiles > cus) {
+      const int64_t halves = (rows + 31) / 32 * ((cols + 63) / 64);
+      if ((halves + cus - 1) / cus < 2 * ((tiles + cus - 1) / cus)) p.size = 32;
     }
   }
   return p;
@@ -562,9 +676,10 @@ void choose_product(const Product& of, void* workspace, hipStream_t s) {
   Job p = {};
   p.lda = of.a.ld;
   p.ldb = of.b.ld;
-  p.a = whole<T>(of.a.p, &p.lda, of.rows, of.depth, &rest, s);
-  p.b = BA ? whole<T>(of.b.p, &p.ldb, of.depth, of.cols, &rest, s)
-           : whole<T>(of.b.p, &p.ldb, of.cols, of.depth, &rest, s);
+  const Packed a = whole<T>(of.a.p, &p.lda, of.rows, of.depth, &rest);
+  const Packed b = BA ? whole<T>(of.b.p, &p.ldb, of.depth, of.cols, &rest)
+                      : whole<T>(of.b.p, &p.ldb, of.cols, of.depth, &rest);
+  pack<T>(a, b, &p.a, &p.b, s);
   p.rows = of.rows;
   p.cols = of.cols;
   p.depth = of.depth;
@@ -576,15 +691,48 @@ void choose_product(const Product& of, void* workspace, hipStream_t s) {
   }
   if (plan.size == 256) launch_tiles<T, BA, 2, 4, 8, 4>(p, plan, of.to, s);
   else if (plan.size == 128) launch_tiles<T, BA, 2, 2, 4, 4>(p, plan, of.to, s);
-  else launch_tiles<T, BA, 2, 2, 2, 2>(p, plan, of.to, s);
+  else if (plan.size == 64) launch_tiles<T, BA, 2, 2, 2, 2>(p, plan, of.to, s);
+  else if constexpr (sizeof(T) == 4) launch_tiles<T, BA, 2, 2, 2, 1>(p, plan, of.to, s);
   if (plan.shares > 1)
     launch("finish", k_finish<T>,
            dim3(static_cast<uint32_t>((p.rows * (p.ld_partial / 8) + kBlock - 1) / kBlock)),
            dim3(kBlock), 0, s, p, plan.shares, of.to);
 }
 
+// Up to this many rows, and B along, the form for few: 16 x 4096 x 4096 in bf16 takes 9.7 us so
+// and 12.4 in tiles with shares, 32 rows in two such fragments 13.4 and in tiles 13.0.
+constexpr int64_t kFew = 16;
+bool is_few(const Product& p) { return !p.b.across && p.rows <= kFew; }
+
+template <typename T, int WAVES>
+void launch_few(const Product& of, hipStream_t s) {
+  Job p = {};
+  p.a = of.a.p;
+  p.b = of.b.p;
+  p.lda = of.a.ld;
+  p.ldb = of.b.ld;
+  p.rows = of.rows;
+  p.cols = of.cols;
+  p.depth = of.depth;
+  launch("product_few", k_product_few<T, WAVES>,
+         dim3(static_cast<uint32_t>((p.cols + 15) / 16)), dim3(64 * WAVES), 0, s, p, of.to);
+}
+
+// As many waves as there are blocks for, up to 16.
+template <typename T>
+void choose_few(const Product& p, hipStream_t s) {
+  constexpr int64_t kDepth = 128 / sizeof(T);
+  if (p.depth > 16 * kDepth) launch_few<T, 16>(p, s);
+  else if (p.depth > 4 * kDepth) launch_few<T, 8>(p, s);
+  else launch_few<T, 4>(p, s);
+}
+
 template <typename T>
 void launch_product(const Product& p, void* workspace, hipStream_t s) {
+  if (is_few(p)) {
+    choose_few<T>(p, s);
+    return;
+  }
   if (p.b.across) choose_product<T, true>(p, workspace, s);
   else choose_product<T, false>(p, workspace, s);
 }
@@ -638,8 +786,9 @@ void launch_gradient(const DenseGradient& a, void* workspace, hipStream_t s) {
   Job p = {};
   p.lda = a.lddy;
   p.ldb = a.ldx;
-  p.a = whole<T>(a.dy, &p.lda, a.tokens, a.outputs, &rest, s);
-  p.b = whole<T>(a.x, &p.ldb, a.tokens, a.inputs, &rest, s);
+  const Packed dy = whole<T>(a.dy, &p.lda, a.tokens, a.outputs, &rest);
+  const Packed x = whole<T>(a.x, &p.ldb, a.tokens, a.inputs, &rest);
+  pack<T>(dy, x, &p.a, &p.b, s);
   p.rows = a.outputs;
   p.cols = a.inputs;
   float *dw = a.dw, *dbias = a.dbias;
@@ -668,6 +817,7 @@ void launch_gradient(const DenseGradient& a, void* workspace, hipStream_t s) {
 }  // namespace
 
 size_t product_bytes(const Product& p) {
+  if (is_few(p)) return 0;
   const int64_t size = size_of(p.type);
   size_t bytes = 0;
   if (!is_whole(p.a.p, p.a.ld, p.rows, p.depth, size)) bytes += packed_bytes(p.rows, p.depth, size);

@@ -62,7 +62,7 @@ class _Gradient(_c.Structure):
 _vp, _i32, _i64, _sz, _f32 = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_size_t, _c.c_float
 _b8 = _c.POINTER(_Block8)
 _counts_p = _c.POINTER(_i64)
-_rb, _gradients_p = _c.POINTER(_ResidualBlock), _c.POINTER(_Gradient)
+_rb = _c.POINTER(_ResidualBlock)
 _SIGNATURES = {
     "garfield_checkpoint": (_i32, [_vp, _i32, _i64, _i64, _i64, _i32, _b8, _vp]),
     "garfield_restore": (_i32, [_b8, _vp, _i32, _i64, _vp]),
@@ -97,10 +97,9 @@ _SIGNATURES = {
                                                _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64,
                                                _i32, _counts_p, _c.POINTER(_ResidualGradients),
                                                _vp, _sz, _vp]),
-    "garfield_clip_workspace": (_sz, [_gradients_p, _i32, _i32]),
-    "garfield_gradient_norms": (_i32, [_gradients_p, _i32, _i32, _vp, _vp, _sz, _vp]),
-    "garfield_clip_gradients": (_i32, [_gradients_p, _i32, _i32, _f32, _vp, _vp, _i64, _vp, _sz,
-                                       _vp]),
+    "garfield_clip_workspace": (_sz, [_vp, _i32, _i32]),
+    "garfield_gradient_norms": (_i32, [_vp, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "garfield_clip_gradients": (_i32, [_vp, _i32, _i32, _f32, _vp, _vp, _i64, _vp, _sz, _vp]),
 }
 _fn = {}
 
@@ -437,7 +436,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
     act = _activation(activation)
     pb = None if bias is None else _vector(bias, "bias", outputs, _WEIGHTS[dtype], dev)
     pr, ldr = _like(residual, "residual", tokens, outputs, x)
-    out = _empty((tokens, outputs), dtype=dtype, device=dev)
+    out = x.new_empty((tokens, outputs))
     kept = torch.empty_like(out) if pre else None
     px, pw, ld = x.data_ptr(), w.data_ptr(), outputs or 1
     ws, need = _workspace("garfield_linear_workspace", dev, px, kind, tokens, inputs, ldx, pw,
@@ -464,7 +463,7 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, pre: torch.Tensor | None 
         raise ValueError("pre and activation go together")
     pp, ldp = _like(pre, "pre", tokens, inputs, dy)
     pr, ldr = _like(residual, "residual", tokens, inputs, dy)
-    dx = _empty((tokens, inputs), dtype=dy.dtype, device=dev)
+    dx = dy.new_empty((tokens, inputs))
     py, pw = dy.data_ptr(), w.data_ptr()
     ws, need = _workspace("garfield_linear_backward_workspace", dev, py, kind, tokens, outputs, ld,
                           pw, inputs, ldw)
@@ -569,16 +568,18 @@ def residual_norm(x: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None 
     normed = weight is not None
     if y8 and not normed:
         raise ValueError("y8 needs a weight")
-    s = _empty((rows, cols), dtype=dtype, device=dev)
+    s = torch.empty_like(x) if ldx == cols else _empty((rows, cols), dtype=dtype, device=dev)
     out = torch.empty_like(s) if y and normed else None
     cy = Checkpoint.empty(rows, cols, dev) if y8 else None
-    held = [normed and not rms, normed, post_weight is not None and not rms,
-            post_weight is not None]
-    flat = iter(_empty((sum(held), rows), dtype=torch.float32, device=dev).unbind(0))
-    stats = [next(flat) if is_held else None for is_held in held]
+    post = post_weight is not None
+    flat = _empty((normed + post) * (1 if rms else 2) * rows, dtype=torch.float32, device=dev)
+    stats, at, places, given = [], flat.data_ptr(), [], 0
+    for there in (normed and not rms, normed, post and not rms, post):
+        stats.append(flat[given:given + rows] if there else None)
+        places.append(at + 4 * given if there else None)
+        given += rows if there else 0
     _run("garfield_residual_norm", dev, _c.byref(b), x.data_ptr(), ldx, ph, ldh, s.data_ptr(),
-         cols, None if out is None else out.data_ptr(), cols,
-         *[None if v is None else v.data_ptr() for v in stats], cy._at if y8 else None)
+         cols, None if out is None else out.data_ptr(), cols, *places, cy._at if y8 else None)
     return ResidualNorm(s, out, cy, *stats)
 
 
@@ -648,7 +649,7 @@ def residual_norm_backward(r: ResidualNorm, h: torch.Tensor, ds: torch.Tensor | 
         sums[name], ld = _rows_of_workers(given, "d" + name, (n, cols), dev)
         setattr(to, name, sums[name].data_ptr())
         setattr(to, "ld_" + name, ld)
-    dx = _empty((rows, cols), dtype=h.dtype, device=dev)
+    dx = torch.empty_like(h) if ldh == cols else _empty((rows, cols), dtype=h.dtype, device=dev)
     dh = torch.empty_like(dx)
     by_tokens = gate is not None and not by_columns
     dg = torch.empty_like(dx) if by_tokens else None
@@ -663,28 +664,28 @@ def residual_norm_backward(r: ResidualNorm, h: torch.Tensor, ds: torch.Tensor | 
 
 def _tensors(grads):
     """The workers' tensors as garfield_clip_gradients takes them: their count, the workers,
-    the C array, the device and the values of a worker."""
+    a C array of garfield_gradient, the device and the values of a worker."""
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
     if not grads:
         raise ValueError("grads must hold a tensor")
-    held = (_Gradient * len(grads))()
-    n, dev, d = None, None, 0
-    for i, g in enumerate(grads):
-        if not isinstance(g, torch.Tensor) or g.dim() < 1 or g.dtype not in TYPES or not g.is_cuda:
+    words, n, d = [], None, 0
+    for g in grads:
+        kind = TYPES.get(g.dtype) if isinstance(g, torch.Tensor) else None
+        if kind is None or g.dim() < 1 or not g.is_cuda:
             raise ValueError("grads must be float32, bfloat16 or float16 tensors on a GPU, "
                              "their first dimension the workers")
-        n, dev = (g.shape[0], g.device) if n is None else (n, dev)
+        if n is None:
+            n, dev = g.shape[0], g.device
         if g.shape[0] != n or g.device != dev or n < 1:
             raise ValueError("grads must have the same workers (one at least) and device")
         length, ld = g.numel() // n, g.stride(0)
-        if n == 1:
-            ld = length
-        if length and not (g.is_contiguous() or (g[0].is_contiguous() and ld >= length)):
+        if not g.is_contiguous() and length and not (
+                (n == 1 or ld >= length) and g[0].is_contiguous()):
             raise ValueError("each worker's values of a tensor must be next to each other, and "
                              "the workers' must not overlap")
-        held[i] = _Gradient(g.data_ptr(), length, ld, TYPES[g.dtype])
+        words += (g.data_ptr(), length, ld if n > 1 else length, kind)  # a _Gradient's
         d += length
-    return len(grads), n, held, dev, d
+    return len(grads), n, (_i64 * len(words))(*words), dev, d
 
 
 def gradient_norms(grads) -> torch.Tensor:

@@ -521,7 +521,9 @@ def _clip_close(got, want, dtype):
 @pytest.mark.parametrize("types", [[F32], [BF16], [F16, F32, BF16]])
 @pytest.mark.parametrize("n,lengths", [(1, [1]), (1, [70000]), (3, [1, 0, 17]), (11, [1000, 7, 130, 65, 9]),
                                        (19, [40000, 3, 16384, 16385]), (64, [33, 5]),
-                                       (2, [1 + 37 * i for i in range(150)]), (5, [300_001, 8])])
+                                       (2, [1 + 37 * i for i in range(150)]), (5, [300_001, 8]),
+                                       (3, [5] * 100), (2, [131072]), (2, [131072, 1]),
+                                       (1, [70_000] * 64), (1, [70_000] * 65), (4, [513, 511, 512])])
 def test_clip_gradients(n, lengths, types):
     grads = _pieces(n, lengths, types, n + len(lengths))
     norms = ref.clip(grads, 1.0)[0]

@@ -151,7 +151,10 @@ def test_clip_refuses(fn):
                                              None)
 
     for bad in (dict(n=0), dict(most=-1.0), dict(most=float("nan")), dict(norms=None), dict(norms=P + 2),
-                dict(out=P + 2), dict(ld=14), dict(ws=None), dict(ws=P + 8), dict(size=8),
+                dict(out=P + 2), dict(ld=14),
+                dict(tensors=((P, 1 << 20, 1 << 20, 0),), ld=1 << 20, ws=None),
+                dict(tensors=((P, 1 << 20, 1 << 20, 0),), ld=1 << 20, ws=P + 8),
+                dict(tensors=((P, 1 << 20, 1 << 20, 0),), ld=1 << 20, size=8),
                 dict(tensors=((None, 10, 10, 0),)), dict(tensors=((P + 2, 10, 10, 0),)),
                 dict(tensors=((P, 10, 9, 0),)), dict(tensors=((P, -1, 10, 0),)), dict(tensors=((P, 10, 10, 3),)),
                 # in place, tensors may not share memory
