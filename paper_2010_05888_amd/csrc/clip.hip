@@ -19,8 +19,7 @@ namespace garfield {
 
 namespace {
 
-constexpr int64_t kChunk = 16384;  // values of a worker's tensor that a workgroup takes
-constexpr int kTable = 64;         // tensors in a launch's arguments
+constexpr int kTable = 64;  // tensors in a launch's arguments
 
 // A tensor, where it goes in a worker's row of the result, and the chunks before it.
 struct Entry {
@@ -37,9 +36,20 @@ __global__ __launch_bounds__(kTable) void k_table(Table part, Entry* __restrict_
   if (static_cast<int>(threadIdx.x) < part.count) to[threadIdx.x] = part.e[threadIdx.x];
 }
 
-// The tensor whose chunk it is; `e` in memory or in the arguments.
+// The tensor whose chunk it is; `e` in memory or in the arguments. Up to 256 are looked at at
+// once (with one reading after the other the norms of 161 tensors took 372 us, not 320).
 template <typename Entries>
 __device__ __forceinline__ int tensor_of(const Entries& e, int count, int64_t chunk) {
+  if (count <= 256) {
+    int at_or_before = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = k * 64 + threadIdx.x % 64;
+      if (k * 64 < count)
+        at_or_before += __builtin_popcountll(__ballot(i < count && e[i < count ? i : 0].chunk <= chunk));
+    }
+    return __builtin_amdgcn_readfirstlane(at_or_before) - 1;
+  }
   int lo = 0, hi = count;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
@@ -60,41 +70,62 @@ __device__ __forceinline__ double add_squares(const typename Pack8<T>::type& v, 
   return sum;
 }
 
+// Values before the first address that is a multiple of 32 bytes, fewer than 16: a worker's row
+// of a tensor starts anywhere, and vectors at any address cost some 15% of the bandwidth.
+template <typename T>
+__device__ __forceinline__ int64_t before_line(const T* p, int64_t length) {
+  const int64_t n = (32 - reinterpret_cast<uintptr_t>(p) % 32) % 32 / sizeof(T);
+  return n < length ? n : length;
+}
+
 // A thread's part of a chunk: four vectors at a time on their way.
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* p, int64_t length) {
   constexpr int64_t kApart = kBlock * 8;
   double sum = 0.0;
+  const int64_t head = before_line(p, length);
+  if (threadIdx.x < head) {
+    const double x = static_cast<double>(static_cast<float>(p[threadIdx.x]));
+    sum = x * x;
+  }
+  p += head;
+  length -= head;
   int64_t i = threadIdx.x * 8;
-  for (; i + 3 * kApart + 8 <= length; i += 4 * kApart) {
+  for (; i - threadIdx.x * 8 + kApart < length; i += 4 * kApart) {
     typename Pack8<T>::type v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = raw8_upto(p + i + k * kApart, 8);
+    for (int k = 0; k < 4; ++k) v[k] = raw8_upto(p + i + k * kApart, length - i - k * kApart);
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum = add_squares<T>(v[k], sum);
   }
-  for (; i < length; i += kApart) sum = add_squares<T>(raw8_upto(p + i, length - i), sum);
+  if (i < length) sum = add_squares<T>(raw8_upto(p + i, length - i), sum);
   return sum;
 }
 
 template <typename T, typename Out>
 __device__ __forceinline__ void chunk_scale(const T* p, int64_t length, float factor, Out* out) {
   constexpr int64_t kApart = kBlock * 8;
+  const int64_t head = before_line(out, length);  // whole lines are written
+  if (threadIdx.x < head)
+    out[threadIdx.x] = static_cast<Out>(static_cast<float>(p[threadIdx.x]) * factor);
+  p += head;
+  out += head;
+  length -= head;
   int64_t i = threadIdx.x * 8;
   float t[8];
-  for (; i + 3 * kApart + 8 <= length; i += 4 * kApart) {
+  for (; i - threadIdx.x * 8 + kApart < length; i += 4 * kApart) {
     typename Pack8<T>::type v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = raw8_upto(p + i + k * kApart, 8);
+    for (int k = 0; k < 4; ++k) v[k] = raw8_upto(p + i + k * kApart, length - i - k * kApart);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       unpack8<T>(v[k], t);
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] *= factor;
-      store8_upto(out + i + k * kApart, 8, t);
+      store8_upto(out + i + k * kApart, length - i - k * kApart, t);
     }
   }
-  for (; i < length; i += kApart) {
+  if (i < length) {
     load8_upto(p + i, length - i, t);
 #pragma unroll
     for (int e = 0; e < 8; ++e) t[e] *= factor;
@@ -131,16 +162,17 @@ __device__ __forceinline__ float factor_of(double norm, float max_norm) {
 template <bool MEMORY>
 __global__ __launch_bounds__(kBlock) void k_squares(Table table, const Entry* __restrict__ more,
                                                     int count, int n, int64_t chunks,
+                                                    int64_t length,
                                                     double* __restrict__ partial) {
   __shared__ double at[kBlock / 64];
   for (int64_t b = blockIdx.x; b < n * chunks; b += gridDim.x) {
     const int64_t worker = b / chunks, chunk = b % chunks;
     const Entry e = MEMORY ? more[tensor_of(more, count, chunk)]
                            : table.e[tensor_of(table.e, count, chunk)];
-    const int64_t first = (chunk - e.chunk) * kChunk, left = e.t.length - first;
+    const int64_t first = (chunk - e.chunk) * length, left = e.t.length - first;
     double sum = 0.0;
     by_type(e.t.values, e.t.type, [&](auto* p) {
-      sum = chunk_squares(p + worker * e.t.ld + first, left < kChunk ? left : kChunk);
+      sum = chunk_squares(p + worker * e.t.ld + first, left < length ? left : length);
     });
     sum = sum_block<kBlock / 64>(sum, at);
     if (threadIdx.x == 0) partial[b] = sum;
@@ -162,19 +194,39 @@ __global__ __launch_bounds__(kBlock) void k_norms(const double* __restrict__ par
   }
 }
 
+// A worker's norm from few chunks is added up by each of its workgroups, and no launch of its own.
+constexpr int64_t kOwnSum = 4 * kBlock;
+
 template <bool MEMORY>
 __global__ __launch_bounds__(kBlock) void k_scale(Table table, const Entry* __restrict__ more,
                                                   int count, int n, int64_t chunks,
+                                                  int64_t most,
+                                                  const double* __restrict__ partial,
+                                                  float max_norm, float* __restrict__ norms,
                                                   const float* __restrict__ factors,
                                                   float* __restrict__ out, int64_t ld_out) {
+  __shared__ double at[kBlock / 64];
   for (int64_t b = blockIdx.x; b < n * chunks; b += gridDim.x) {
     const int64_t worker = b / chunks, chunk = b % chunks;
-    const float factor = factors[worker];
+    float factor;
+    if (chunks <= kOwnSum) {
+      double sum = 0.0;
+#pragma unroll
+      for (int k = 0; k < kOwnSum / kBlock; ++k) {
+        const int64_t c = k * kBlock + threadIdx.x;
+        if (c < chunks) sum += partial[worker * chunks + c];
+      }
+      const double norm = __builtin_sqrt(sum_block<kBlock / 64>(sum, at));
+      factor = factor_of(norm, max_norm);
+      if (chunk == 0 && threadIdx.x == 0) norms[worker] = static_cast<float>(norm);
+    } else {
+      factor = factors[worker];
+    }
     if (!out && factor == 1.0f) continue;
     const Entry e = MEMORY ? more[tensor_of(more, count, chunk)]
                            : table.e[tensor_of(table.e, count, chunk)];
-    const int64_t first = (chunk - e.chunk) * kChunk, left = e.t.length - first;
-    const int64_t length = left < kChunk ? left : kChunk;
+    const int64_t first = (chunk - e.chunk) * most, left = e.t.length - first;
+    const int64_t length = left < most ? left : most;
     by_type(e.t.values, e.t.type, [&](auto* p) {
       p += worker * e.t.ld + first;
       if (out) chunk_scale(p, length, factor, out + worker * ld_out + e.at + first);
@@ -183,10 +235,10 @@ __global__ __launch_bounds__(kBlock) void k_scale(Table table, const Entry* __re
   }
 }
 
-// All of it in one launch, a workgroup a worker, where a worker has few values: its waves take
-// chunks of 512 in turn, four at a time on their way, and read them again when the norm is known.
-// 11 workers' 100,000 values in six tensors take 9 us, in three launches 5.4 + 2.4 + 6.7.
-constexpr int64_t kFew = 131072;
+// All of it in one launch, a workgroup a worker, where a worker has few values of one type: its
+// waves take chunks of 512 in turn, four at a time on their way, and read them again when the
+// norm is known. (A CU has no more than some 60 GB/s so: 11 workers' 100,000 values take 20 us.)
+constexpr int64_t kFew = 16384;
 constexpr int kFewWaves = 16;
 struct FewTable {
   int count;
@@ -194,85 +246,88 @@ struct FewTable {
   garfield_gradient t[kTable];
   int64_t at[kTable];
 };
+template <typename T>
 __global__ __launch_bounds__(64 * kFewWaves) void k_clip_few(FewTable table, float max_norm,
                                                              float* __restrict__ norms,
-                                                             float* __restrict__ out,
-                                                             int64_t ld_out, bool norms_alone) {
+                                                             float* out, int64_t ld_out,
+                                                             bool norms_alone) {
   constexpr int kAtOnce = 4;
   __shared__ double at[kFewWaves];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int64_t worker = blockIdx.x;
   const int chunks = table.first[table.count];
-  // four chunks' values: f(k, tensor, the lane's first value in it, how many are there, values)
+  // f(tensor, the lane's first value of a chunk, how many are there from it on, eight of them)
   auto each = [&](auto&& f) {
     int tensor = 0;
     for (int c0 = wave; c0 < chunks; c0 += kFewWaves * kAtOnce) {
-      float v[kAtOnce][8];
-      int of[kAtOnce];
-      int64_t from[kAtOnce], left[kAtOnce];
+      typename Pack8<T>::type v[kAtOnce];
+      int of[kAtOnce], from[kAtOnce], left[kAtOnce];
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
-        const int c = c0 + k * kFewWaves;
-        of[k] = -1;
-        if (c >= chunks) continue;
+        const int c = c0 + k * kFewWaves < chunks ? c0 + k * kFewWaves : chunks - 1;
         while (c >= table.first[tensor + 1]) ++tensor;
         const garfield_gradient& t = table.t[tensor];
         of[k] = tensor;
-        from[k] = int64_t{c - table.first[tensor]} * 512 + lane * 8;
-        left[k] = t.length - from[k];
-        by_type(t.values, t.type, [&](auto* p) {
-          load8_upto(p + worker * t.ld + from[k], left[k], v[k]);
-        });
+        from[k] = (c - table.first[tensor]) * 512 + lane * 8;
+        left[k] = c == c0 + k * kFewWaves ? static_cast<int>(t.length) - from[k] : 0;
+        v[k] = raw8_upto(static_cast<const T*>(t.values) + worker * t.ld + from[k], left[k]);
       }
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k)
-        if (of[k] >= 0 && left[k] > 0) f(of[k], from[k], left[k], v[k]);
+      for (int k = 0; k < kAtOnce; ++k) f(of[k], from[k], left[k], v[k]);
     }
   };
   double sum = 0.0;
-  each([&](int, int64_t, int64_t, float* v) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      sum = __builtin_fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum);
-  });
+  each([&](int, int, int, const typename Pack8<T>::type& v) { sum = add_squares<T>(v, sum); });
   const double norm = __builtin_sqrt(sum_block<kFewWaves>(sum, at));
   if (threadIdx.x == 0) norms[worker] = static_cast<float>(norm);
   const float factor = factor_of(norm, max_norm);
   if (norms_alone || (!out && factor == 1.0f)) return;
-  each([&](int tensor, int64_t from, int64_t left, float* v) {
+  each([&](int tensor, int from, int left, const typename Pack8<T>::type& v) {
+    float t[8];
+    unpack8<T>(v, t);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= factor;
-    const garfield_gradient& t = table.t[tensor];
+    for (int e = 0; e < 8; ++e) t[e] *= factor;
     if (out)
-      store8_upto(out + worker * ld_out + table.at[tensor] + from, left, v);
+      store8_upto(out + worker * ld_out + table.at[tensor] + from, left, t);
     else
-      by_type(t.values, t.type, [&](auto* p) { store8_upto(p + worker * t.ld + from, left, v); });
+      store8_upto(static_cast<T*>(table.t[tensor].values) + worker * table.t[tensor].ld + from, left,
+                  t);
   });
 }
 
-int64_t chunks_of(const garfield_gradient& t) { return (t.length + kChunk - 1) / kChunk; }
+int64_t chunks_of(const garfield_gradient& t, int64_t length) {
+  return (t.length + length - 1) / length;
+}
 
-// Tensors that hold values, their chunks and a worker's values.
+// Tensors that hold values, a worker's values, their type (-1: several), and the chunks.
 struct Totals {
-  int count;
-  int64_t chunks, values;
+  int count, type;
+  int64_t values, length, chunks;  // length: of a chunk
 };
-Totals totals(const garfield_gradient* tensors, int count) {
-  Totals all = {0, 0, 0};
+Totals totals(const garfield_gradient* tensors, int count, int n) {
+  Totals all = {};
   for (int i = 0; i < count; ++i) {
-    all.count += tensors[i].length > 0;
-    all.chunks += chunks_of(tensors[i]);
+    if (tensors[i].length == 0) continue;
+    all.type = all.count == 0 || all.type == tensors[i].type ? tensors[i].type : -1;
+    ++all.count;
     all.values += tensors[i].length;
   }
+  // as long as there are four chunks for a CU, up to 16384 (chunks of 65536: 19 workers'
+  // 25,557,032 values 45 us more)
+  all.length = 16384;
+  while (all.length > 2048 && n * all.values < all.length * 4 * device_cus()) all.length /= 2;
+  for (int i = 0; i < count; ++i) all.chunks += chunks_of(tensors[i], all.length);
   return all;
 }
 
-bool is_few(const Totals& all) { return all.count <= kTable && all.values <= kFew; }
+bool is_few(const Totals& all) {
+  return all.count <= kTable && all.values <= kFew && all.type >= 0;
+}
 
 }  // namespace
 
 size_t clip_bytes(const garfield_gradient* tensors, int count, int n) {
-  const Totals all = totals(tensors, count);
+  const Totals all = totals(tensors, count, n);
   if (is_few(all)) return 0;
   return static_cast<size_t>(n) * all.chunks * sizeof(double) +
          (all.count > kTable ? all.count * sizeof(Entry) : 0) + n * sizeof(float);
@@ -280,7 +335,7 @@ size_t clip_bytes(const garfield_gradient* tensors, int count, int n) {
 
 hipError_t enqueue_clip(const garfield_gradient* tensors, int count, int n, float max_norm,
                         float* norms, float* out, int64_t ld_out, void* workspace, hipStream_t s) {
-  const Totals all = totals(tensors, count);
+  const Totals all = totals(tensors, count, n);
   const bool norms_alone = max_norm != max_norm;
   if (is_few(all)) {
     FewTable few = {};
@@ -293,8 +348,11 @@ hipError_t enqueue_clip(const garfield_gradient* tensors, int count, int n, floa
       few.first[k + 1] = few.first[k] + static_cast<int>((tensors[i].length + 511) / 512);
       at += tensors[i].length;
     }
-    launch("clip_few", k_clip_few, dim3(n), dim3(64 * kFewWaves), 0, s, few, max_norm, norms, out,
-           ld_out, norms_alone);
+    launch("clip_few",
+           all.type == GARFIELD_F32    ? k_clip_few<float>
+           : all.type == GARFIELD_BF16 ? k_clip_few<__bf16>
+                                       : k_clip_few<_Float16>,
+           dim3(n), dim3(64 * kFewWaves), 0, s, few, max_norm, norms, out, ld_out, norms_alone);
     return hipGetLastError();
   }
   double* partial = static_cast<double*>(workspace);
@@ -313,7 +371,7 @@ hipError_t enqueue_clip(const garfield_gradient* tensors, int count, int n, floa
     if (table.count == kTable) flush();
     table.e[table.count++] = {tensors[i], at, chunk};
     at += tensors[i].length;
-    chunk += chunks_of(tensors[i]);
+    chunk += chunks_of(tensors[i], all.length);
   }
   const bool memory = all.count > kTable;
   if (memory && table.count > 0) flush();
@@ -321,12 +379,14 @@ hipError_t enqueue_clip(const garfield_gradient* tensors, int count, int n, floa
   const int64_t groups = std::min(n * all.chunks, int64_t{1} << 23);
   const dim3 grid(static_cast<uint32_t>(groups));
   launch("squares", memory ? k_squares<true> : k_squares<false>, grid, dim3(kBlock), 0, s, table,
-         static_cast<const Entry*>(more), all.count, n, all.chunks, partial);
-  launch("norms", k_norms, dim3(n), dim3(kBlock), 0, s, static_cast<const double*>(partial),
-         all.chunks, max_norm, norms, factors);
+         static_cast<const Entry*>(more), all.count, n, all.chunks, all.length, partial);
+  if (norms_alone || all.chunks > kOwnSum)
+    launch("norms", k_norms, dim3(n), dim3(kBlock), 0, s, static_cast<const double*>(partial),
+           all.chunks, max_norm, norms, factors);
   if (!norms_alone)
     launch("scale", memory ? k_scale<true> : k_scale<false>, grid, dim3(kBlock), 0, s, table,
-           static_cast<const Entry*>(more), all.count, n, all.chunks,
+           static_cast<const Entry*>(more), all.count, n, all.chunks, all.length,
+           static_cast<const double*>(partial), max_norm, norms,
            static_cast<const float*>(factors), out, ld_out);
   return hipGetLastError();
 }

@@ -525,25 +525,27 @@ class ResidualNorm(NamedTuple):
 
 def _residual_block(like: torch.Tensor, rows, cols, kind, weight, bias, post_weight, post_bias,
                     gate, scale, eps, rms):
-    dev, dtype = like.device, like.dtype
-    wtype, pointers = None, {}
+    dev, allowed = like.device, _WEIGHTS[like.dtype]
     if rms and (bias is not None or post_bias is not None):
         raise ValueError("with rms a norm has no bias")
     if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
         raise ValueError("a bias needs its weight")
-    vectors = {"weight": weight, "bias": bias, "post_weight": post_weight, "post_bias": post_bias}
-    if gate is not None and isinstance(gate, torch.Tensor) and gate.dim() == 1:
-        vectors["gate"] = gate
-    for name, v in vectors.items():
-        if v is not None:
-            pointers[name] = _vector(v, name, cols, _WEIGHTS[dtype] if wtype is None else (wtype,),
-                                     dev)
-            wtype = v.dtype
+    by_columns = isinstance(gate, torch.Tensor) and gate.dim() == 1
+    wtype, pointers = None, []
+    for name, v in (("weight", weight), ("bias", bias), ("post_weight", post_weight),
+                    ("post_bias", post_bias), ("gate", gate if by_columns else None)):
+        if v is None:
+            pointers.append(None)
+        else:
+            pointers.append(_vector(v, name, cols, allowed, dev))
+            if wtype is None:  # the others' too
+                wtype = v.dtype
+                allowed = (wtype,)
     ld_gate = 0
-    if gate is not None and "gate" not in vectors:
-        pointers["gate"], ld_gate = _like(gate, "gate", rows, cols, like)
-    return _ResidualBlock(kind, TYPES[wtype or torch.float32], rows, cols, 1 if rms else 0, eps,
-                          scale, ld_gate=ld_gate, **pointers)
+    if gate is not None and not by_columns:
+        pointers[4], ld_gate = _like(gate, "gate", rows, cols, like)
+    return _ResidualBlock(kind, 0 if wtype is None else TYPES[wtype], rows, cols, 1 if rms else 0,
+                          eps, scale, *pointers, ld_gate)
 
 
 def residual_norm(x: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None = None,
@@ -572,14 +574,12 @@ def residual_norm(x: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None 
     out = torch.empty_like(s) if y and normed else None
     cy = Checkpoint.empty(rows, cols, dev) if y8 else None
     post = post_weight is not None
-    flat = _empty((normed + post) * (1 if rms else 2) * rows, dtype=torch.float32, device=dev)
-    stats, at, places, given = [], flat.data_ptr(), [], 0
-    for there in (normed and not rms, normed, post and not rms, post):
-        stats.append(flat[given:given + rows] if there else None)
-        places.append(at + 4 * given if there else None)
-        given += rows if there else 0
+    held = [normed and not rms, normed, post and not rms, post]
+    flat = iter(_empty((sum(held), rows), dtype=torch.float32, device=dev).unbind(0))
+    stats = [next(flat) if there else None for there in held]
     _run("garfield_residual_norm", dev, _c.byref(b), x.data_ptr(), ldx, ph, ldh, s.data_ptr(),
-         cols, None if out is None else out.data_ptr(), cols, *places, cy._at if y8 else None)
+         cols, None if out is None else out.data_ptr(), cols,
+         *[None if v is None else v.data_ptr() for v in stats], cy._at if y8 else None)
     return ResidualNorm(s, out, cy, *stats)
 
 
@@ -635,20 +635,23 @@ def residual_norm_backward(r: ResidualNorm, h: torch.Tensor, ds: torch.Tensor | 
     by_columns = gate is not None and gate.dim() == 1
     if dgate is not None and not by_columns:
         raise ValueError("dgate is given for a gate of columns only")
-    there = {"weight": (dweight, weight is not None), "bias": (dbias, weight is not None and not rms),
-             "post_weight": (dpost_weight, post_weight is not None),
-             "post_bias": (dpost_bias, post_weight is not None and not rms),
-             "gate": (dgate, by_columns)}
-    to, sums = _ResidualGradients(), {}
-    for name, (given, asked) in there.items():
-        if not asked:
-            if given is not None:
-                raise ValueError(f"d{name} was given, but there is no such parameter")
-            sums[name] = None
-            continue
-        sums[name], ld = _rows_of_workers(given, "d" + name, (n, cols), dev)
-        setattr(to, name, sums[name].data_ptr())
-        setattr(to, "ld_" + name, ld)
+    biased = not rms
+    sums, pointers, apart = [], [], []
+    for name, given, there in (
+            ("dweight", dweight, weight is not None), ("dbias", dbias, biased and weight is not None),
+            ("dpost_weight", dpost_weight, post_weight is not None),
+            ("dpost_bias", dpost_bias, biased and post_weight is not None),
+            ("dgate", dgate, by_columns)):
+        ld = pointer = None
+        if there:
+            given, ld = _rows_of_workers(given, name, (n, cols), dev)
+            pointer = given.data_ptr()
+        elif given is not None:
+            raise ValueError(f"{name} was given, but there is no such parameter")
+        sums.append(given)
+        pointers.append(pointer)
+        apart.append(ld or 0)
+    to = _ResidualGradients(*pointers, *apart)
     dx = torch.empty_like(h) if ldh == cols else _empty((rows, cols), dtype=h.dtype, device=dev)
     dh = torch.empty_like(dx)
     by_tokens = gate is not None and not by_columns
@@ -658,8 +661,9 @@ def residual_norm_backward(r: ResidualNorm, h: torch.Tensor, ds: torch.Tensor | 
     _run("garfield_residual_norm_backward", dev, at, pds, ldds, pdy, lddy, ps, lds, h.data_ptr(),
          ldh, *stats, dx.data_ptr(), cols, dh.data_ptr(), cols, dg.data_ptr() if by_tokens else None,
          cols, n, counts, _c.byref(to), ws.data_ptr() if need else None, need)
-    return ResidualNormBackward(dx, dh, sums["weight"], sums["bias"], sums["post_weight"],
-                                sums["post_bias"], dg if by_tokens else sums["gate"])
+    if by_tokens:
+        sums[4] = dg
+    return ResidualNormBackward(dx, dh, *sums)
 
 
 def _tensors(grads):
