@@ -410,6 +410,9 @@ def _like(v, name: str, rows: int, cols: int, x: torch.Tensor):
     """The pointer and row distance of a matrix of x's type and device (None: none)."""
     if v is None:
         return None, 0
+    if (isinstance(v, torch.Tensor) and v.dtype is x.dtype and v.shape == (rows, cols)
+            and v.is_contiguous() and v.device == x.device):
+        return v.data_ptr(), cols  # as _matrix and what follows it find, in a third of the time
     r, c, ld, _ = _matrix(v, name, x.dtype)
     if (r, c) != (rows, cols) or v.device != x.device:
         raise ValueError(f"{name} must be {rows} x {cols} on {x.device}")
@@ -530,22 +533,25 @@ def _residual_block(like: torch.Tensor, rows, cols, kind, weight, bias, post_wei
         raise ValueError("with rms a norm has no bias")
     if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
         raise ValueError("a bias needs its weight")
-    by_columns = isinstance(gate, torch.Tensor) and gate.dim() == 1
-    wtype, pointers = None, []
-    for name, v in (("weight", weight), ("bias", bias), ("post_weight", post_weight),
-                    ("post_bias", post_bias), ("gate", gate if by_columns else None)):
-        if v is None:
-            pointers.append(None)
-        else:
-            pointers.append(_vector(v, name, cols, allowed, dev))
-            if wtype is None:  # the others' too
-                wtype = v.dtype
-                allowed = (wtype,)
+    wtype = pw = pb = ppw = ppb = pg = None
     ld_gate = 0
-    if gate is not None and not by_columns:
-        pointers[4], ld_gate = _like(gate, "gate", rows, cols, like)
+    if weight is not None:
+        pw, wtype = _vector(weight, "weight", cols, allowed, dev), weight.dtype
+        allowed = (wtype,)  # the others' too
+        if bias is not None:
+            pb = _vector(bias, "bias", cols, allowed, dev)
+    if post_weight is not None:
+        ppw, wtype = _vector(post_weight, "post_weight", cols, allowed, dev), post_weight.dtype
+        allowed = (wtype,)
+        if post_bias is not None:
+            ppb = _vector(post_bias, "post_bias", cols, allowed, dev)
+    if gate is not None:
+        if isinstance(gate, torch.Tensor) and gate.dim() == 1:
+            pg, wtype = _vector(gate, "gate", cols, allowed, dev), gate.dtype
+        else:
+            pg, ld_gate = _like(gate, "gate", rows, cols, like)
     return _ResidualBlock(kind, 0 if wtype is None else TYPES[wtype], rows, cols, 1 if rms else 0,
-                          eps, scale, *pointers, ld_gate)
+                          eps, scale, pw, pb, ppw, ppb, pg, ld_gate)
 
 
 def residual_norm(x: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None = None,
@@ -574,13 +580,22 @@ def residual_norm(x: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None 
     out = torch.empty_like(s) if y and normed else None
     cy = Checkpoint.empty(rows, cols, dev) if y8 else None
     post = post_weight is not None
-    held = [normed and not rms, normed, post and not rms, post]
-    flat = iter(_empty((sum(held), rows), dtype=torch.float32, device=dev).unbind(0))
-    stats = [next(flat) if there else None for there in held]
+    flat = _empty(((normed + post) * (1 if rms else 2), rows), dtype=torch.float32, device=dev)
+    at, apart, mean, post_mean = flat.data_ptr(), 4 * rows, None, None
+    left = iter(flat.unbind(0))  # in the order of their places
+    places = [None] * 4
+    if normed:
+        if not rms:
+            mean, places[0], at = next(left), at, at + apart
+        rstd, places[1], at = next(left), at, at + apart
+    if post:
+        if not rms:
+            post_mean, places[2], at = next(left), at, at + apart
+        post_rstd, places[3] = next(left), at
     _run("garfield_residual_norm", dev, _c.byref(b), x.data_ptr(), ldx, ph, ldh, s.data_ptr(),
-         cols, None if out is None else out.data_ptr(), cols,
-         *[None if v is None else v.data_ptr() for v in stats], cy._at if y8 else None)
-    return ResidualNorm(s, out, cy, *stats)
+         cols, None if out is None else out.data_ptr(), cols, *places, cy._at if y8 else None)
+    return ResidualNorm(s, out, cy, mean, rstd if normed else None, post_mean,
+                        post_rstd if post else None)
 
 
 class ResidualNormBackward(NamedTuple):
