@@ -2,6 +2,7 @@
 // gradient of its input, and of each worker the gradient of its weights.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "activation.h"
 #include "block8.h"
@@ -24,11 +25,14 @@ struct Finish {
   static __device__ __forceinline__ Raw raw(const void* p, int64_t at) {
     return *reinterpret_cast<const Raw*>(static_cast<const T*>(p) + at);
   }
-  static __device__ __forceinline__ void store(void* p, int64_t at, const float* v) {
+  static __device__ __forceinline__ void store(const Epilogue& e, void* p, int64_t at,
+                                               const float* v) {
     Raw t;
 #pragma unroll
     for (int i = 0; i < N; ++i) t[i] = static_cast<T>(v[i]);
-    *reinterpret_cast<Raw*>(static_cast<T*>(p) + at) = t;
+    Raw* const to = reinterpret_cast<Raw*>(static_cast<T*>(p) + at);
+    if (e.past_caches) __builtin_nontemporal_store(t, to);
+    else *to = t;
   }
 
   __device__ __forceinline__ void ask(const Epilogue& e, int64_t m, int64_t j) {
@@ -55,14 +59,14 @@ struct Finish {
           for (int i = 0; i < N; ++i) v[i] += static_cast<float>(t[i]);
         }
       }
-      if (e.pre) store(e.pre, m * e.ld_pre + j, v);
+      if (e.pre) store(e, e.pre, m * e.ld_pre + j, v);
       activate<N>(e.activation, v);
     }
     if (e.residual) {
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += static_cast<float>(residual[i]);
     }
-    store(e.out, m * e.ld_out + j, v);
+    store(e, e.out, m * e.ld_out + j, v);
   }
 
   // What is there of eight outputs, one after the other.
@@ -80,8 +84,9 @@ struct Finish {
 };
 
 // Workgroup id to tile: workgroups go to the eight XCDs in turn, so an XCD's
-// share is made contiguous, and inside it eight tiles of rows deep: the tiles that
-// an XCD has in work share their rows of both operands in its L2.
+// share is made contiguous, and inside it four tiles of rows deep: the tiles that
+// an XCD has in work share their rows of both operands in its L2, and write next to each
+// other (eight deep, 16384 x 8192 x 2048 takes 484 us, so 470; weight gradients below).
 // `parts`: shares of the depth, or workers, whose tiles come one part after the other.
 struct Place {
   int64_t m, j;
@@ -89,7 +94,7 @@ struct Place {
 };
 __device__ __forceinline__ Place place_of(uint32_t id, uint32_t total, uint32_t tiles_m,
                                           uint32_t tiles_j) {
-  constexpr uint32_t kXcds = 8, kDeep = 8;
+  constexpr uint32_t kXcds = 8, kDeep = 4;
   const uint32_t share = total / kXcds, more = total % kXcds, xcd = id % kXcds;
   uint32_t at = xcd * share + (xcd < more ? xcd : more) + id / kXcds;
   const int part = static_cast<int>(at / (tiles_m * tiles_j));
@@ -207,34 +212,41 @@ struct Tile {
     barrier();  // LDS is free
   }
 
-  // Every output of the first `lines` x `columns`, eight neighbouring ones of a line at a time:
-  // ask(state, line, column), and some lines later put(state, line, column, values); the line's
-  // last ones, fewer than eight, some(line, column, how many, value by number). A lane has four
-  // columns of one line in each of its sums; by way of the wave's own part of LDS, `kPass` sums
-  // at a time, they become lines of FA * 16 columns: a line's even 16-byte pieces, then its odd
-  // ones, piece p of these at p ^ line % kSwap. So 16 lanes that write a piece of 16 lines, or
-  // read every other piece of one, have banks of their own.
-  template <typename State, typename Ask, typename Put, typename Some>
+  // Every output of the first `lines` x `columns`, N neighbouring ones of a line at a time, 16
+  // bytes of the result: ask(state, line, column), and some lines later put(state, line, column,
+  // values); the line's last ones, fewer than N, some(line, column, how many, value by number). A
+  // lane has four columns of one line in each of its sums; by way of the wave's own part of LDS,
+  // `kPass` sums at a time, they become lines of FA * 16 columns, in 16-byte pieces: for N = 8 the
+  // even ones, then the odd ones. Piece p lies at p ^ line % kSwap. So 16 lanes that write a piece
+  // of 16 lines, or read 16 pieces (every other one) of a line, have banks of their own.
+  // (Eight fp32 values a lane, in two stores of 16 bytes each: 19 workers' 16384 x 2048 x 8192 took
+  // 710 us, four with every store whole lines 668.)
+  template <int N, typename State, typename Ask, typename Put, typename Some>
   static __device__ __forceinline__ void rows_of(uint8_t* lds, const v4f (&sum)[FA][FB],
                                                  int64_t lines, int64_t columns, Ask&& ask,
                                                  Put&& put, Some&& some) {
     constexpr int kLine = FA * 64, kRoom = 2 * kStage / kWaves;
     constexpr int kPass = kRoom / (16 * kLine) < FB ? kRoom / (16 * kLine) : FB;
-    constexpr int kEights = FA * 2, kSwap = FA * 4 < 16 ? FA * 4 : 16, kApart = 64 / kEights;
+    constexpr int kInLine = FA * 16 / N, kSwap = FA * 4 < 16 ? FA * 4 : 16, kApart = 64 / kInLine;
     constexpr int kSteps = kPass * 16 / kApart;  // of a pass
     constexpr int kAsked = kSteps % 2 == 0 ? 2 : 1;
-    static_assert(kPass > 0 && FB % kPass == 0, "equal parts");
+    static_assert(kPass > 0 && FB % kPass == 0 && (N == 4 || N == 8), "equal parts");
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wj = wave / WM, wm = wave % WM;
     uint8_t* const own = lds + wave * kRoom;
-    const int first = lane / kEights, c = lane % kEights, column = wj * FA * 16 + c * 8;
+    const int first = lane / kInLine, c = lane % kInLine, column = wj * FA * 16 + c * N;
     const int here = lines < kRows ? static_cast<int>(lines) : kRows;
-    const int left = columns - column < 8 ? static_cast<int>(columns - column) : 8;
+    const int left = columns - column < N ? static_cast<int>(columns - column) : N;
+    // where piece p of a line lies
+    auto place = [](int p, int line) {
+      const int at = N == 8 ? p / 2 + FA * 2 * (p % 2) : p;
+      return line * kLine + (at ^ (line % kSwap)) * 16;
+    };
     State state[kAsked];
 #pragma unroll
     for (int q = 0; q < kAsked; ++q) {
       const int line = wm * FB * 16 + first + q * kApart;
-      if (left == 8 && line < here) ask(state[q], line, column);
+      if (left == N && line < here) ask(state[q], line, column);
     }
 #pragma unroll
     for (int k0 = 0; k0 < FB; k0 += kPass) {
@@ -242,9 +254,7 @@ struct Tile {
       for (int k = 0; k < kPass; ++k)
 #pragma unroll
         for (int i = 0; i < FA; ++i)
-          *reinterpret_cast<v4f*>(
-              own + (k * 16 + lane % 16) * kLine +
-              ((i * 2 + lane / 32 + kEights * (lane / 16 % 2)) ^ (lane % kSwap)) * 16) =
+          *reinterpret_cast<v4f*>(own + place(i * 4 + lane / 16, k * 16 + lane % 16)) =
               sum[i][k0 + k];
 #pragma unroll 1
       for (int r0 = first; r0 < kPass * 16; r0 += kAsked * kApart) {
@@ -252,18 +262,17 @@ struct Tile {
         for (int q = 0; q < kAsked; ++q) {
           const int r = r0 + q * kApart, line = (wm * FB + k0) * 16 + r;
           if (line >= here || left <= 0) continue;
-          auto half = [&](int e) {
-            return reinterpret_cast<const float*>(own + r * kLine +
-                                                  ((c + kEights * e) ^ (r % kSwap)) * 16);
+          auto piece = [&](int e) {
+            return reinterpret_cast<const float*>(own + place(c * (N / 4) + e, r));
           };
-          if (left < 8) {
-            some(line, column, left, [&](int e) { return half(e / 4)[e % 4]; });
+          if (left < N) {
+            some(line, column, left, [&](int e) { return piece(e / 4)[e % 4]; });
             continue;
           }
-          float t[8];
+          float t[N];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const v4f v = *reinterpret_cast<const v4f*>(half(e));
+          for (int e = 0; e < N / 4; ++e) {
+            const v4f v = *reinterpret_cast<const v4f*>(piece(e));
 #pragma unroll
             for (int f = 0; f < 4; ++f) t[e * 4 + f] = v[f];
           }
@@ -288,6 +297,14 @@ struct Job {
 
 struct Nothing {};
 
+template <bool PAST_CACHES = false>
+__device__ __forceinline__ void store_four(float* to, const float* v) {
+  typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+  const Four t = {v[0], v[1], v[2], v[3]};
+  if constexpr (PAST_CACHES) __builtin_nontemporal_store(t, reinterpret_cast<Four*>(to));
+  else *reinterpret_cast<Four*>(to) = t;
+}
+
 template <typename T, bool AA, bool BA, int WJ, int WM, int FA, int FB>
 __global__ __launch_bounds__(64 * WJ * WM) void k_product(Job p, Epilogue to) {
   typedef Tile<T, AA, BA, WJ, WM, FA, FB> Of;
@@ -302,22 +319,23 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_product(Job p, Epilogue to) {
   Of::sums(lds, p.lda, p.ldb, parts, sum, [](auto&) {});
   if (p.partial) {  // whose lines go on to whole eights
     float* const out = p.partial + at.part * p.rows * p.ld_partial + m0 * p.ld_partial + j0;
-    Of::template rows_of<Nothing>(
+    Of::template rows_of<4, Nothing>(
         lds, sum, parts.rows, (parts.cols + 7) / 8 * 8, [](Nothing&, int, int) {},
         [&](const Nothing&, int line, int column, float* v) {
-          store8_upto(out + line * p.ld_partial + column, 8, v);
+          store_four(out + line * p.ld_partial + column, v);
         },
         [](int, int, int, auto&&) {});
   } else {
-    typedef Finish<T, 8> Eight;
-    Of::template rows_of<Eight>(
+    constexpr int kPiece = 16 / sizeof(T);
+    typedef Finish<T, kPiece> Piece;
+    Of::template rows_of<kPiece, Piece>(
         lds, sum, parts.rows, parts.cols,
-        [&](Eight& f, int line, int column) { f.ask(to, m0 + line, j0 + column); },
-        [&](const Eight& f, int line, int column, float* v) {
+        [&](Piece& f, int line, int column) { f.ask(to, m0 + line, j0 + column); },
+        [&](const Piece& f, int line, int column, float* v) {
           f.put(to, m0 + line, j0 + column, v);
         },
         [&](int line, int column, int left, auto&& value) {
-          Eight::some(to, m0 + line, j0 + column, left, value);
+          Piece::some(to, m0 + line, j0 + column, left, value);
         });
   }
 }
@@ -450,7 +468,8 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_dense_gradient(Job p, Workers 
                                                                  float* __restrict__ dw,
                                                                  int64_t ld_dw,
                                                                  float* __restrict__ dbias,
-                                                                 int64_t ld_dbias) {
+                                                                 int64_t ld_dbias,
+                                                                 bool whole_lines) {
   typedef Tile<T, true, true, WJ, WM, FA, FB> Of;
   __shared__ __align__(1024) uint8_t lds[2 * Of::kStage];
   const Place at = place_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_j);
@@ -487,16 +506,23 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_dense_gradient(Job p, Workers 
       if (m < p.rows) dbias[at.part * ld_dbias + m] = ones[k][0];
     }
   }
+  // Whole lines go past the caches: with 19 workers' 16384 x 4096 x 4096 680 us by way of them and
+  // 600 past them, with 11 workers' 1000 tokens 180 and 144. (Lines of several tiles of one row
+  // next to each other matter too: four tiles deep 16384 x 2048 x 8192 takes 640, eight 680.)
   float* const out = dw + at.part * ld_dw + m0 * p.cols + j0;
-  Of::template rows_of<Nothing>(
-      lds, sum, parts.rows, parts.cols, [](Nothing&, int, int) {},
-      [&](const Nothing&, int line, int column, float* v) {
-        store8_upto(out + line * p.cols + column, 8, v);
-      },
-      [&](int line, int column, int left, auto&& value) {
+  auto store = [&](auto past_caches) {
+    Of::template rows_of<4, Nothing>(
+        lds, sum, parts.rows, parts.cols, [](Nothing&, int, int) {},
+        [&](const Nothing&, int line, int column, float* v) {
+          store_four<decltype(past_caches)::value>(out + line * p.cols + column, v);
+        },
+        [&](int line, int column, int left, auto&& value) {
 #pragma unroll 1
-        for (int e = 0; e < left; ++e) out[line * p.cols + column + e] = value(e);
-      });
+          for (int e = 0; e < left; ++e) out[line * p.cols + column + e] = value(e);
+        });
+  };
+  if (whole_lines) store(std::true_type());
+  else store(std::false_type());
 }
 
 // The splits' gradients added in ascending order: `length` values for each of n workers,
@@ -670,6 +696,12 @@ void launch_tiles(Job p, const Plan& plan, const Epilogue& to, hipStream_t s) {
          dim3(p.tiles_m * p.tiles_j * plan.shares), dim3(64 * WJ * WM), 0, s, p, to);
 }
 
+// Whether the matrix's rows are whole lines, which are stored past the caches: 16384 x 8192 x 2048
+// with gelu and p takes 518 us so and 536 by way of them. Parts of lines stay for the others.
+bool whole_lines(const void* p, int64_t ld, int64_t size) {
+  return reinterpret_cast<uintptr_t>(p) % 128 == 0 && ld * size % 128 == 0;
+}
+
 template <typename T, bool BA>
 void choose_product(const Product& of, void* workspace, hipStream_t s) {
   char* rest = static_cast<char*>(workspace);
@@ -684,19 +716,23 @@ void choose_product(const Product& of, void* workspace, hipStream_t s) {
   p.cols = of.cols;
   p.depth = of.depth;
   const Plan plan = plan_product(p.rows, p.cols, p.depth, sizeof(T));
+  Epilogue to = of.to;
+  to.past_caches = whole_lines(to.out, to.ld_out, sizeof(T)) &&
+                   (!to.pre || whole_lines(to.pre, to.ld_pre, sizeof(T)));
   p.share = plan.share;
   if (plan.shares > 1) {
+    to.past_caches = false;  // k_finish
     p.partial = reinterpret_cast<float*>(rest);
     p.ld_partial = up_to(p.cols, 8);
   }
-  if (plan.size == 256) launch_tiles<T, BA, 2, 4, 8, 4>(p, plan, of.to, s);
-  else if (plan.size == 128) launch_tiles<T, BA, 2, 2, 4, 4>(p, plan, of.to, s);
-  else if (plan.size == 64) launch_tiles<T, BA, 2, 2, 2, 2>(p, plan, of.to, s);
-  else if constexpr (sizeof(T) == 4) launch_tiles<T, BA, 2, 2, 2, 1>(p, plan, of.to, s);
+  if (plan.size == 256) launch_tiles<T, BA, 2, 4, 8, 4>(p, plan, to, s);
+  else if (plan.size == 128) launch_tiles<T, BA, 2, 2, 4, 4>(p, plan, to, s);
+  else if (plan.size == 64) launch_tiles<T, BA, 2, 2, 2, 2>(p, plan, to, s);
+  else if constexpr (sizeof(T) == 4) launch_tiles<T, BA, 2, 2, 2, 1>(p, plan, to, s);
   if (plan.shares > 1)
     launch("finish", k_finish<T>,
            dim3(static_cast<uint32_t>((p.rows * (p.ld_partial / 8) + kBlock - 1) / kBlock)),
-           dim3(kBlock), 0, s, p, plan.shares, of.to);
+           dim3(kBlock), 0, s, p, plan.shares, to);
 }
 
 // Up to this many rows, and B along, the form for few: 16 x 4096 x 4096 in bf16 takes 9.7 us so
@@ -756,6 +792,8 @@ void launch_gradients(Job p, const Workers& w, float* dw, int64_t ld_dw, float* 
                       int64_t ld_dbias, hipStream_t s) {
   p.tiles_m = static_cast<uint32_t>((p.rows + WM * FB * 16 - 1) / (WM * FB * 16));
   p.tiles_j = static_cast<uint32_t>((p.cols + WJ * FA * 16 - 1) / (WJ * FA * 16));
+  const bool whole_lines =
+      reinterpret_cast<uintptr_t>(dw) % 128 == 0 && ld_dw % 32 == 0 && p.cols % 32 == 0;
   // A launch has fewer than 2^32 threads: many workers' tiles may take several
   const int64_t tiles = int64_t{p.tiles_m} * p.tiles_j * w.splits;
   const int fit = static_cast<int>(std::min<int64_t>(0xffffffff / (64 * WJ * WM) / tiles, w.n));
@@ -765,7 +803,7 @@ void launch_gradients(Job p, const Workers& w, float* dw, int64_t ld_dw, float* 
     for (int k = 0; k <= some.n; ++k) some.first[k] = w.first[i + k];
     launch("dense_gradient", k_dense_gradient<T, WJ, WM, FA, FB>,
            dim3(static_cast<uint32_t>(tiles * some.n)), dim3(64 * WJ * WM), 0, s, p, some,
-           dw + i * ld_dw, ld_dw, dbias ? dbias + i * ld_dbias : nullptr, ld_dbias);
+           dw + i * ld_dw, ld_dw, dbias ? dbias + i * ld_dbias : nullptr, ld_dbias, whole_lines);
   }
 }
 

@@ -93,6 +93,7 @@ struct Epilogue {
   int64_t ld_out = 0;
   void* pre = nullptr;
   int64_t ld_pre = 0;
+  bool past_caches = false;  // how out and pre are stored
 };
 struct Operand {
   const void* p = nullptr;
