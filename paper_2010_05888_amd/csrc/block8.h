@@ -40,7 +40,12 @@ __device__ __forceinline__ typename Pack8<T>::type raw8_upto(const T* p, int64_t
   if (left >= 8) return *reinterpret_cast<const typename Pack8<T>::type*>(p);
   typename Pack8<T>::type t;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) t[e] = e < left ? p[e] : static_cast<T>(0.0f);
+  for (int e = 0; e < 8; ++e) t[e] = static_cast<T>(0.0f);
+  if (left > 0) {  // lanes past the row's end are many, and pass by
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) t[e] = p[e];
+  }
   return t;
 }
 
@@ -55,7 +60,12 @@ __device__ __forceinline__ void load8(const T* p, float* v) {
 template <typename T>
 __device__ __forceinline__ void load8_tail(const T* p, int64_t left, float* v) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = e < left ? static_cast<float>(p[e]) : 0.0f;
+  for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+  if (left > 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) v[e] = static_cast<float>(p[e]);
+  }
 }
 
 template <typename T>
@@ -71,7 +81,7 @@ __device__ __forceinline__ void store8_upto(T* p, int64_t left, const float* v) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) t[e] = static_cast<T>(v[e]);
     *reinterpret_cast<typename Pack8<T>::type*>(p) = t;
-  } else {
+  } else if (left > 0) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < left) p[e] = static_cast<T>(v[e]);

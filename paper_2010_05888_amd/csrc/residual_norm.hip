@@ -74,15 +74,19 @@ __device__ __forceinline__ void long_statistics(const garfield_residual_block& b
     double sum = 0.0;
     for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
       values(c, v);
-      for (int e = 0; e < 8 && c + e < b.cols; ++e) sum += v[e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += c + e < b.cols ? v[e] : 0.0f;
     }
     *mean = static_cast<float>(sum_group<kLongWaves>(sum, totals) * share);
   }
   float square = 0.0f;
   for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
     values(c, v);
-    for (int e = 0; e < 8 && c + e < b.cols; ++e)
-      square = __builtin_fmaf(v[e] - *mean, v[e] - *mean, square);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float t = c + e < b.cols ? v[e] - *mean : 0.0f;
+      square = __builtin_fmaf(t, t, square);
+    }
   }
   square = sum_group<kLongWaves>(square, sums);
   *rstd = 1.0f / __builtin_sqrtf(square * static_cast<float>(share) + b.eps);
@@ -335,7 +339,9 @@ __device__ __forceinline__ void backward_sums(const ResidualNormBackward& a, int
   for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
     backward_values<T>(a, row, c, 0.0f, 0.0f, t);
     load_parameter<T>(b.weight, b.wtype == GARFIELD_F32, c, b.cols - c, 1.0f, w);
-    for (int e = 0; e < 8 && c + e < b.cols; ++e) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (c + e >= b.cols) continue;
       x = __builtin_fmaf(t.dy[e], w[e], x);
       y = __builtin_fmaf(t.dy[e] * w[e], t.hat[e], y);
     }
@@ -361,7 +367,9 @@ __global__ __launch_bounds__(kLong) void k_residual_dx_long(ResidualNormBackward
     for (int64_t c = threadIdx.x * 8; c < b.cols; c += kLong * 8) {
       backward_values<T>(a, row, c, along, across, t);
       load_parameter<T>(b.post_weight, f32, c, b.cols - c, 1.0f, w);
-      for (int e = 0; e < 8 && c + e < b.cols; ++e) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (c + e >= b.cols) continue;
         x = __builtin_fmaf(t.df[e], w[e], x);
         y = __builtin_fmaf(t.df[e] * w[e], t.post[e], y);
       }
@@ -396,7 +404,9 @@ constexpr int kSums = 5;
 // share of the parameters' gradients in registers, and writes that to `partial`;
 // k_residual_sums adds the chunks of a worker. R rows are worked on at a time, with one
 // barrier for each norm's sums, while the next R are on their way.
-// HOLD: the parameters stay in registers, else they are read again for every R rows.
+// HOLD: the parameters and all sums stay in registers and the next rows' ds and gate come early
+// too; else the parameters are read again for every R rows, ds and the gate come under the first
+// norm's sums, and all sums but the first live in LDS, each thread's own values.
 template <typename T, int THREADS, int NV, int R, bool HOLD>
 __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackward a,
                                                                Chunks chunks, int sums_of,
@@ -404,6 +414,8 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
   constexpr int kWaves = THREADS / 64;
   typedef typename Pack8<T>::type Raw;
   __shared__ float sums[2][2][kWaves][2 * R];
+  constexpr int kHeld = HOLD ? kSums : 1;  // sums in registers
+  __shared__ v4f totals[HOLD ? 1 : kSums - 1][NV][2][HOLD ? 1 : THREADS];
   const garfield_residual_block& b = a.b;
   const int chunk = blockIdx.x, worker = worker_of(chunks, chunk);
   const int64_t begin = chunks.token0[worker] + (chunk - chunks.chunk0[worker]) * chunks.rows;
@@ -412,7 +424,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
   const float scale = 1.0f / static_cast<float>(b.cols);
   const bool f32 = b.wtype == GARFIELD_F32, by_tokens = b.gate && b.ld_gate;
   const bool post = b.post_weight != nullptr;
-  float w[NV][8], pw[NV][8], pb[NV][8], gv[NV][8], total[kSums][NV][8];
+  float w[NV][8], pw[NV][8], pb[NV][8], gv[NV][8], total[kHeld][NV][8];
   auto parameter = [&](const void* p, float missing, float (&v)[NV][8]) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -430,9 +442,35 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
 #pragma unroll
   for (int k = 0; k < kSums; ++k)
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
+      if (k < kHeld) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) total[k][j][e] = 0.0f;
+        for (int e = 0; e < 8; ++e) total[k < kHeld ? k : 0][j][e] = 0.0f;
+      } else {
+        totals[k - kHeld][j][0][threadIdx.x] = totals[k - kHeld][j][1][threadIdx.x] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+  // x * y (y null: x) of eight columns added to sum k
+  auto add = [&](int k, int j, const float* x, const float* y) {
+    if (k < kHeld) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float& t = total[k < kHeld ? k : 0][j][e];
+        t = y ? __builtin_fmaf(x[e], y[e], t) : t + x[e];
+      }
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        v4f t = totals[k - kHeld][j][half][threadIdx.x];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = half * 4 + e;
+          t[e] = y ? __builtin_fmaf(x[i], y[i], t[e]) : t[e] + x[i];
+        }
+        totals[k - kHeld][j][half][threadIdx.x] = t;
+      }
+    }
+  };
   Raw ds[R][NV], dy[R][NV], s[R][NV], h[R][NV], gate[R][NV];
   float mean[R], rstd[R], post_mean[R], post_rstd[R];
 #pragma unroll
@@ -466,9 +504,24 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
           dy[r][j] = of(a.dy, a.lddy);
           s[r][j] = of(a.s, a.lds);
         }
-        if (a.ds) ds[r][j] = of(a.ds, a.ldds);
         h[r][j] = of(a.h, a.ldh);
-        if (by_tokens) gate[r][j] = of(b.gate, b.ld_gate);
+        if constexpr (HOLD) {
+          if (a.ds) ds[r][j] = of(a.ds, a.ldds);
+          if (by_tokens) gate[r][j] = of(b.gate, b.ld_gate);
+        }
+      }
+    }
+  };
+  auto fetch_late = [&](int64_t row0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = row0 + r < end ? row0 + r : end - 1;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+        if (a.ds) ds[r][j] = raw8_upto(static_cast<const T*>(a.ds) + row * a.ldds + c, left);
+        if (by_tokens)
+          gate[r][j] = raw8_upto(static_cast<const T*>(b.gate) + row * b.ld_gate + c, left);
       }
     }
   };
@@ -478,7 +531,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
     float g[R][NV][8], hat[R][NV][8], z[R][NV][8], k[R][NV][8], both[2 * R], d[R], pd[R];
     if constexpr (!HOLD) {
       parameter(b.weight, 0.0f, w);
-      parameter(columns, 1.0f, gv);
+      fetch_late(row0);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -492,17 +545,18 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
         unpack8<T>(dy[r][j], g[r][j]);
         unpack8<T>(s[r][j], hat[r][j]);
         unpack8<T>(h[r][j], z[r][j]);
-        if (by_tokens) unpack8<T>(gate[r][j], k[r][j]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if (!by_tokens) k[r][j][e] = gv[j][e];
           hat[r][j][e] = (hat[r][j][e] - mean[r]) * d[r];
           if (post) z[r][j][e] = (z[r][j][e] - post_mean[r]) * pd[r];
           if (left < 8 && e >= left) hat[r][j][e] = z[r][j][e] = 0.0f;
-          if (there) {
-            total[0][j][e] = __builtin_fmaf(g[r][j][e], hat[r][j][e], total[0][j][e]);
-            total[1][j][e] += g[r][j][e];
-          }
+        }
+        if (there) {
+          add(0, j, g[r][j], hat[r][j]);
+          if (HOLD || sums_of & 2) add(1, j, g[r][j], nullptr);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
           g[r][j][e] *= w[j][e];
           along += g[r][j][e];
           across = __builtin_fmaf(g[r][j][e], hat[r][j][e], across);
@@ -511,15 +565,28 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
       both[2 * r] = along;
       both[2 * r + 1] = across;
     }
-    // ds goes on to the whole gradient, and the next rows come
+    // ds and the gate go on to the whole gradient, and the next rows come
     float more[R][NV][8];
+    auto go_on = [&] {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int j = 0; j < NV; ++j) unpack8<T>(ds[r][j], more[r][j]);
+        for (int j = 0; j < NV; ++j) {
+          unpack8<T>(ds[r][j], more[r][j]);
+          if (by_tokens) {
+            unpack8<T>(gate[r][j], k[r][j]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[r][j][e] = gv[j][e];
+          }
+        }
+    };
+    if constexpr (HOLD) go_on();
     if (row0 + R < end) fetch(row0 + R);
     if (a.dy) sums_group<kWaves, 2 * R>(both, sums[0][odd]);
     if constexpr (!HOLD) {
+      parameter(columns, 1.0f, gv);
+      go_on();
       parameter(b.post_weight, 1.0f, pw);
       parameter(b.post_bias, 0.0f, pb);
     }
@@ -542,11 +609,14 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
           f[e] = post ? __builtin_fmaf(z[r][j][e], pw[j][e], pb[j][e]) : z[r][j][e];
           f[e] *= v;
           k[r][j][e] *= v;  // the gradient of N_post(h)
-          if (there) {
-            total[2][j][e] = __builtin_fmaf(k[r][j][e], z[r][j][e], total[2][j][e]);
-            total[3][j][e] += k[r][j][e];
-            total[4][j][e] += f[e];
-          }
+        }
+        if (there) {
+          if (HOLD || sums_of & 4) add(2, j, k[r][j], z[r][j]);
+          if (HOLD || sums_of & 8) add(3, j, k[r][j], nullptr);
+          if (HOLD || sums_of & 16) add(4, j, f, nullptr);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
           if (post) {
             k[r][j][e] *= pw[j][e];
             x += k[r][j][e];
@@ -588,7 +658,15 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int64_t c = (j * THREADS + threadIdx.x) * 8;
-      if (c < b.cols) store8_upto(out + c, b.cols - c, total[q][j]);
+      if (c >= b.cols) continue;
+      if (q < kHeld) {
+        store8_upto(out + c, b.cols - c, total[q < kHeld ? q : 0][j]);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = totals[q - kHeld][j][e / 4][threadIdx.x][e % 4];
+        store8_upto(out + c, b.cols - c, v);
+      }
     }
   }
 }
@@ -689,7 +767,7 @@ void choose_backward(const ResidualNormBackward& a, const Chunks& c, void* works
                dim3(static_cast<uint32_t>((cols + 511) / 512), c.chunk0[c.n]), dim3(64), 0, s, a, c,
                means, sums, partial);
     } else if (cols > 4096) {
-      launch_backward<T, 1024, 1, 1, false>(a, c, partial, s);
+      launch_backward<T, 512, 2, 1, false>(a, c, partial, s);
     } else if (cols > 2048) {
       launch_backward<T, 512, 1, 1>(a, c, partial, s);
     } else if (cols > 1024) {
@@ -725,11 +803,14 @@ void choose_forward(const ResidualNorm& a, hipStream_t s) {
     launch("residual_norm_long", k_residual_norm_long<T>, dim3(static_cast<uint32_t>(a.b.rows)),
            dim3(kLong), 0, s, a);
   else if (cols > 8192) launch_forward<T, 16, 2, 1>(a, s);
-  else if (cols > 4096) launch_forward<T, 4, 4, 1>(a, s);
+  else if (cols > 6144) launch_forward<T, 8, 2, 1>(a, s);
+  else if (cols > 4096) launch_forward<T, 12, 1, 1>(a, s);
   else if (many && cols > 2048) launch_forward<T, 4, 2, 2>(a, s);
   else if (many && cols > 1024) launch_forward<T, 4, 1, 2>(a, s);
   else if (cols > 2048) launch_forward<T, 4, 2, 1>(a, s);
   else if (cols > 1024) launch_forward<T, 4, 1, 1>(a, s);
+  else if (many && cols > 512) launch_forward<T, 1, 2, 2>(a, s);
+  else if (many) launch_forward<T, 1, 1, 4>(a, s);
   else if (cols > 512) launch_forward<T, 1, 2, 1>(a, s);
   else launch_forward<T, 1, 1, 1>(a, s);
 }
