@@ -181,21 +181,20 @@ bool tensors_ok(const garfield_gradient* t, int count, int n) {
   return true;
 }
 
+// A tensor's bytes: n rows of `length`, `apart` apart.
+struct Range {
+  uintptr_t first, end;
+  uintptr_t apart, length;
+};
+Range range_of(const garfield_gradient& t, int n) {
+  const uintptr_t b = element_bytes(t.type), p = reinterpret_cast<uintptr_t>(t.values);
+  const uintptr_t apart = n > 1 ? t.ld * b : 0, length = t.length * b;
+  return {p, p + apart * (n - 1) + length, apart, length};
+}
+
 // Whether no two of the tensors have a byte in common. Tensors whose ranges overlap may still
 // be columns of one matrix: rows equally far apart, and no columns shared.
-bool tensors_apart(const garfield_gradient* t, int count, int n) {
-  struct Range {
-    uintptr_t first, end;
-    uintptr_t apart, length;  // bytes
-  };
-  std::vector<Range> all;
-  all.reserve(count);
-  for (int i = 0; i < count; ++i) {
-    if (t[i].length == 0) continue;
-    const uintptr_t b = element_bytes(t[i].type), p = reinterpret_cast<uintptr_t>(t[i].values);
-    const uintptr_t apart = n > 1 ? t[i].ld * b : 0, length = t[i].length * b;
-    all.push_back({p, p + apart * (n - 1) + length, apart, length});
-  }
+bool ranges_apart(std::vector<Range>& all, int n) {
   std::sort(all.begin(), all.end(), [](const Range& x, const Range& y) { return x.first < y.first; });
   // In a group of ranges that overlap, all must be columns of the first one's matrix: its
   // rows, in which no column starts before the last one's end, and which wrap round once.
@@ -210,6 +209,30 @@ bool tensors_apart(const garfield_gradient* t, int count, int n) {
       end = std::max(end, all[k].end);
     }
     i = k;
+  }
+  return true;
+}
+
+bool tensors_apart(const garfield_gradient* t, int count, int n) {
+  std::vector<Range> all;
+  all.reserve(count);
+  for (int i = 0; i < count; ++i)
+    if (t[i].length > 0) all.push_back(range_of(t[i], n));
+  return ranges_apart(all, n);
+}
+
+// Whether none of them has a byte in common with the rows that are written.
+bool apart_from(const garfield_gradient* t, int count, int n, float* out, int64_t d, int64_t ld) {
+  const garfield_gradient rows = {out, d, ld, GARFIELD_F32};
+  const Range to = range_of(rows, n);
+  std::vector<Range> both(2);
+  for (int i = 0; i < count; ++i) {
+    if (t[i].length == 0) continue;
+    const Range r = range_of(t[i], n);
+    if (r.end <= to.first || to.end <= r.first) continue;
+    both[0] = r;
+    both[1] = to;
+    if (!ranges_apart(both, n)) return false;
   }
   return true;
 }
@@ -653,12 +676,11 @@ garfield_status garfield_clip_gradients(const garfield_gradient* tensors, int co
   if (!tensors_ok(tensors, count, n) || !vector_ok(norms, 4, n) || !gradient_ok(out, n, d, ld_out) ||
       !workspace_ok(workspace, workspace_bytes, clip_bytes(tensors, count, n)))
     return GARFIELD_EINVAL;
-  if (!out) {
-    try {
-      if (!tensors_apart(tensors, count, n)) return GARFIELD_EINVAL;
-    } catch (const std::bad_alloc&) {
-      return GARFIELD_ENOMEM;
-    }
+  try {
+    if (out ? !apart_from(tensors, count, n, out, d, ld_out) : !tensors_apart(tensors, count, n))
+      return GARFIELD_EINVAL;
+  } catch (const std::bad_alloc&) {
+    return GARFIELD_ENOMEM;
   }
   return status_of(enqueue_clip(tensors, count, n, max_norm, norms, out, ld_out, workspace,
                                 static_cast<hipStream_t>(stream)));

@@ -194,6 +194,11 @@ def test_products_of_subnormal_and_largest_values():
     w = torch.full((8, 64), 1024.0, dtype=F16)
     got = gf.linear(x.to(DEV), w.to(DEV)).out
     assert torch.equal(got.cpu(), torch.full((40, 8), 64 * 2.0 ** -14, dtype=F16))
+    for dtype in (F32, BF16):  # subnormal factors of a normal product, in tiles and for few rows
+        for rows in (3, 40):
+            x = torch.full((rows, 64), 2.0 ** -130, dtype=dtype)
+            got = gf.linear(x.to(DEV), w.to(dtype).to(DEV)).out
+            assert torch.equal(got.cpu(), torch.full((rows, 8), 2.0 ** -114, dtype=dtype))
     for dtype in (F32, BF16):
         top = torch.finfo(dtype).max
         x = torch.zeros(40, 64, dtype=dtype)
@@ -484,6 +489,26 @@ def test_residual_norm_gradients_against_differences():
             close(getattr(got, "d" + k), want, 3e-5 * want.abs().max() * torch.ones_like(want), k)
 
 
+@pytest.mark.parametrize("cols", [300, 5000, 9000])
+def test_residual_norm_backward_from_one_gradient(cols):
+    """Without dy the norm after passes nothing on and its weight's gradient is 0; without ds the
+    rest is as with a ds of zeros."""
+    rows, counts = 12, [5, 7]
+    s, h, g = (_rand(rows, cols, i).to(DEV) for i in range(3))
+    block = _moved(_block(rows, cols, F32))
+    block.pop("bias")
+    stats = [0.1 * torch.ones(rows, device=DEV), torch.ones(rows, device=DEV)] * 2
+    r = gf.ResidualNorm(s, None, None, *stats)
+
+    def call(ds, dy):
+        return gf.residual_norm_backward(r, h, ds, dy, **block, counts=counts)
+
+    for a, b in ((call(g, None), call(g, torch.zeros_like(g))), (call(None, g), call(torch.zeros_like(g), g))):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+    assert not bool(call(g, None).dweight.any()) and torch.equal(call(g, None).dx, g)
+
+
 def test_residual_norm_backward_keeps_what_is_not_finite_with_its_worker():
     rows, cols, counts = 40, 300, [10, 0, 25, 5]
     s, h, ds, dy = (_rand(rows, cols, i) for i in range(4))
@@ -569,6 +594,14 @@ def test_clip_refuses_tensors_that_share_memory():
         with pytest.raises(gf.GarfieldError):
             gf.clip_gradients(parts, 1.0)
         assert bool((m == 1).all())
+    # nor may the rows that are written, but for columns of the same matrix beside them
+    wide = torch.ones(4, 200, device=DEV)
+    for parts, out in (([wide[:, :100]], wide[:, :100]), ([wide[:, :60], wide[:, 160:]], wide[:, 50:150]),
+                       ([wide.view(1, 800)[:, :200]], wide.view(1, 800)[:, 199:399])):
+        with pytest.raises(gf.GarfieldError):
+            gf.clip_gradients(parts, 1.0, out=out)
+    gf.clip_gradients([wide[:, :60], wide[:, 160:]], 1.0, out=wide[:, 60:160])
+    close(wide[:, 60:160], torch.full((4, 100), 0.1), torch.full((4, 100), 2 * U * 0.1))
     assert gf.gradient_norms([m, m]).tolist() == pytest.approx([math.sqrt(200)] * 4)  # reading is fine
 
 

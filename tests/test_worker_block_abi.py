@@ -163,7 +163,11 @@ def test_clip_refuses(fn):
                 dict(out=None, tensors=((P, 10, 30, 0), (P + 40, 21, 30, 0))),
                 dict(out=None, tensors=((P, 10, 30, 0), (P + 40, 10, 31, 0))),
                 dict(out=None, tensors=((P, 10, 30, 0), (P + 40, 10, 60, 1), (P + 56, 5, 30, 0))),
-                dict(out=None, n=1, tensors=((P, 10, 0, 0), (P + 39, 10, 0, 1)))):
+                dict(out=None, n=1, tensors=((P, 10, 0, 0), (P + 39, 10, 0, 1))),
+                # nor with the rows that are written
+                dict(out=P, ld=10, tensors=((P, 10, 10, 0),)), dict(out=P + 36, ld=30, tensors=((P, 10, 30, 0),)),
+                dict(out=P + 40, ld=31, tensors=((P, 10, 30, 0),)),
+                dict(out=0x9000 + 8, ld=15), dict(out=P - 40, ld=30, tensors=((P, 11, 30, 0),))):
         assert call(**bad) == gf.EINVAL, bad
     assert call(n=65) == gf.ETOOBIG
     assert call(tensors=((P, (1 << 34) + 1, 1 << 35, 0),)) == gf.ETOOBIG
