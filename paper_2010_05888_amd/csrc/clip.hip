@@ -4,8 +4,8 @@
 // one order: lane by lane, wave by wave, chunk by chunk.
 //
 // Bound by memory: a value is read for the norm, and read and written for its clipped one. 19
-// workers' 25,557,032 values take 305 us for the norms (6.4 TB/s) and 775 for the rest (5.0, as a
-// copy). The norm comes first, and a worker's row is behind the caches when it is known: taking
+// workers' 25,557,032 values in 161 tensors take 350 us for the norms (5.5 TB/s) and 777 for the
+// rest (5.0, as a copy). 11 workers' 100,000 values take 3.8 + 5.8 us, latency. The norm comes first, and a worker's row is behind the caches when it is known: taking
 // the workers one after the other, 102 MB each, was no faster (1339 against 1115 us).
 
 #include <algorithm>
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kTable) void k_table(Table part, Entry* __restrict_
 }
 
 // The tensor whose chunk it is; `e` in memory or in the arguments. Up to 256 are looked at at
-// once (with one reading after the other the norms of 161 tensors took 372 us, not 320).
+// once, more one after the other.
 template <typename Entries>
 __device__ __forceinline__ int tensor_of(const Entries& e, int count, int64_t chunk) {
   if (count <= 256) {
@@ -71,14 +71,15 @@ __device__ __forceinline__ double add_squares(const typename Pack8<T>::type& v, 
 }
 
 // Values before the first address that is a multiple of 32 bytes, fewer than 16: a worker's row
-// of a tensor starts anywhere, and vectors at any address cost some 15% of the bandwidth.
+// of a tensor starts anywhere.
 template <typename T>
 __device__ __forceinline__ int64_t before_line(const T* p, int64_t length) {
   const int64_t n = (32 - reinterpret_cast<uintptr_t>(p) % 32) % 32 / sizeof(T);
   return n < length ? n : length;
 }
 
-// A thread's part of a chunk: four vectors at a time on their way.
+// A thread's part of a chunk: four vectors at a time on their way, at its end too (one by one
+// there, the norms took 365 us).
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* p, int64_t length) {
   constexpr int64_t kApart = kBlock * 8;

@@ -1,5 +1,15 @@
 // Products of 16- and 32-bit matrices with an epilogue: a linear layer's forward pass, the
 // gradient of its input, and of each worker the gradient of its weights.
+//
+// All three are A B^T with the depth along or across each operand (dense.h), in one kernel's
+// three forms: X W^T, dY W with W across, and dY^T X with both across and a worker's tokens as
+// its depth. Products are those of the values as they are, sums fp32: fp32 on its own matrix
+// instruction, at a sixteenth of the 16-bit ones' rate.
+//
+// Bounds: the matrix cores' rate, and power (8192^3 in bf16: 800 us, 1370 TFLOP/s; in fp32 7500
+// us, 147 TFLOP/s of 157), and then what an epilogue reads, computes and writes, which no products
+// hide: 16384 x 8192 x 2048 takes 475 us, with gelu and p 535, back through gelu 540, of which
+// 268 MB more at a copy's rate are 51. For one token B's bytes, for small sizes latency.
 
 #include <algorithm>
 #include <type_traits>
@@ -116,11 +126,13 @@ struct Parts {
 // one half it reads the next one's operands, so that nothing but the one barrier of a block, in
 // its middle, is waited for: there the block has been read, and the one after the next starts on
 // its way to its place, a load between every few products, straight to LDS.
-// 8192^3 in bf16: 800 us, 1370 TFLOP/s (a library's product 705), of zeros 700 (530): power bounds
-// both, then the loads' issue (100 us) and the barrier (50). What was slower: waves of 128 x 128,
-// one a SIMD (1220); a block's loads in its first half's products (815); one workgroup for many
-// tiles, the next one's first block on its way during the epilogue (564 against 535 us for 16384 x
-// 8192 x 2048 with gelu and p: its loads wait for its stores; a new workgroup's do not).
+// 8192^3 in bf16: 800 us, 1370 TFLOP/s (a library's product 705 to 790), of zeros 650 (530): power
+// bounds both; the matrix cores are busy 74% of the time, what they wait for are the loads' issue
+// (100 us) and the barrier (50). LDS is read 29% of the time and no bank is waited for. What was
+// slower: waves of 128 x 128, one a SIMD (1220); a block's loads all in its first products (815);
+// one workgroup for many tiles, the next one's first block on its way during the epilogue (564
+// against 535 us for 16384 x 8192 x 2048 with gelu and p: its loads wait for its stores; a new
+// workgroup's do not).
 template <typename T, bool AA, bool BA, int WJ, int WM, int FA, int FB>
 struct Tile {
   static constexpr int kWaves = WJ * WM, kCols = WJ * FA * 16, kRows = WM * FB * 16;

@@ -12,6 +12,18 @@ rules take:
     dx, _, _ = layernorm_backward(dy, r.x8, r.mean, r.rstd, weight, counts, dweight=..., dbias=...)
     aggregate, sel = gar("multikrum", grads, f)
 
+and for a residual block in 16 or 32 bits:
+
+    h = linear(x, w0).out
+    r = residual_norm(x, h, gain, post_weight=post, gate=gate, rms=True)
+    up = linear(r.y, w1, b1, "gelu", pre=True)
+    out = linear(up.out, w2, residual=r.s).out
+    dp = linear_backward(dout, w2, up.pre, "gelu")
+    dw1, _ = linear_weight_gradient(dp, r.y, counts)       # and of w2, w0 alike
+    b = residual_norm_backward(r, h, dout, linear_backward(dp, w1), gain, post, gate=gate,
+                               rms=True, counts=counts)
+    norms = clip_gradients([dw1, b.dweight, ...], max_norm, out=grads)
+
 Nothing here takes part in torch's autograd: a backward pass is called like a
 forward pass.
 
@@ -690,19 +702,21 @@ def _tensors(grads):
     words, n, d = [], None, 0
     for g in grads:
         kind = TYPES.get(g.dtype) if isinstance(g, torch.Tensor) else None
-        if kind is None or g.dim() < 1 or not g.is_cuda:
+        shape = () if kind is None else g.shape
+        if len(shape) < 1 or not g.is_cuda:
             raise ValueError("grads must be float32, bfloat16 or float16 tensors on a GPU, "
                              "their first dimension the workers")
         if n is None:
-            n, dev = g.shape[0], g.device
-        if g.shape[0] != n or g.device != dev or n < 1:
+            n, dev, index = shape[0], g.device, g.get_device()
+        if shape[0] != n or n < 1 or g.get_device() != index:
             raise ValueError("grads must have the same workers (one at least) and device")
-        length, ld = g.numel() // n, g.stride(0)
-        if not g.is_contiguous() and length and not (
-                (n == 1 or ld >= length) and g[0].is_contiguous()):
-            raise ValueError("each worker's values of a tensor must be next to each other, and "
-                             "the workers' must not overlap")
-        words += (g.data_ptr(), length, ld if n > 1 else length, kind)  # a _Gradient's
+        length = ld = g.numel() // n
+        if not g.is_contiguous() and length:
+            ld = g.stride(0) if n > 1 else length
+            if ld < length or not g[0].is_contiguous():
+                raise ValueError("each worker's values of a tensor must be next to each other, "
+                                 "and the workers' must not overlap")
+        words += (g.data_ptr(), length, ld, kind)  # a _Gradient's
         d += length
     return len(grads), n, (_i64 * len(words))(*words), dev, d
 
