@@ -134,3 +134,29 @@ def test_largest_grids_of_thin_matrices():
     r = gf.residual_norm(x, x, torch.ones(3, device=DEV))
     assert bool(r.s.eq(2).all()) and not bool(r.y.any())
     assert bool(gf.activation_backward(x, x, "relu").eq(1).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 16, 17, 61, 130, 5000])
+@pytest.mark.parametrize("pitch,cols", [(1, 1), (1, 0), (3, 2), (5, 5), (7, 6), (8, 7), (9, 9)])
+def test_matrices_that_end_with_their_memory(rows, pitch, cols, dtype):
+    """Rows shorter than a block of depth (pitch and columns in 16-byte pieces, 0: three values),
+    whose last one ends where a block of memory of its own does: nothing behind it is there."""
+    piece = 16 // dtype.itemsize
+    cols, ld = cols * piece or 3, pitch * piece
+
+    def at_end(seed):
+        memory = torch.empty((20 << 20) // dtype.itemsize, dtype=dtype, device=DEV)
+        first = memory.numel() - (rows - 1) * ld - cols
+        view = memory.as_strided((rows, cols), (ld, 1), first)
+        view.copy_(_gpu(rows, cols, seed, dtype))
+        return view
+
+    x, w = at_end(1), at_end(2)
+    _check(gf.linear(x, w).out, ref.linear(x, w, None, None, None)[0], dtype, "product")
+    y = _gpu(rows, rows, 3, dtype)
+    _check(gf.linear_backward(y, w), ref.linear_backward(y, w, None, None, None), dtype, "dx")
+    dw, db = gf.linear_weight_gradient(x, w, dbias=torch.empty(1, cols, device=DEV))
+    want = ref.weight_gradient(x, w, [rows])
+    _check(dw, want[:2], F32, "dw")
+    _check(db, want[2:], F32, "db")
