@@ -5,8 +5,8 @@
 // = q(2 v), and gelu itself u = log(Phi(p) / Phi(-p)), which is p times a polynomial in p^2 to
 // what fp32 shows. One exponential and one reciprocal, each off by a unit or so in the last
 // place, make p q(u) right to 3 u (1 + |p|), u = 2^-24, and gelu's small values at p < 0 to 2^-13
-// of themselves down to p = -6, where they are 6e-9; q below 2^-126 is 0. A product's epilogue has no time to spare:
-// with 134 million outputs gelu by erfc took 91 us more than this does.
+// of themselves down to p = -6, where they are 6e-9; q below 2^-126 is 0. A product's epilogue has
+// no time to spare: with 134 million outputs gelu by erfc took 91 us more than this does.
 #pragma once
 
 #include <hip/hip_runtime.h>

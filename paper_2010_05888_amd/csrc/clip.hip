@@ -5,8 +5,9 @@
 //
 // Bound by memory: a value is read for the norm, and read and written for its clipped one. 19
 // workers' 25,557,032 values in 161 tensors take 350 us for the norms (5.5 TB/s) and 777 for the
-// rest (5.0, as a copy). 11 workers' 100,000 values take 3.8 + 5.8 us, latency. The norm comes first, and a worker's row is behind the caches when it is known: taking
-// the workers one after the other, 102 MB each, was no faster (1339 against 1115 us).
+// rest (5.0, as a copy). 11 workers' 100,000 values take 3.8 + 5.6 us, latency. The norm comes
+// first, and a worker's row is behind the caches when it is known: taking the workers one after the
+// other, 102 MB each, was no faster (1339 against 1115 us).
 
 #include <algorithm>
 
@@ -59,7 +60,7 @@ __device__ __forceinline__ int tensor_of(const Entries& e, int count, int64_t ch
   return lo;
 }
 
-// v's first `left` values of eight squared and added.
+// v's eight values squared and added.
 template <typename T>
 __device__ __forceinline__ double add_squares(const typename Pack8<T>::type& v, double sum) {
 #pragma unroll

@@ -353,7 +353,7 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_product(Job p, Epilogue to) {
 }
 
 // Few rows (up to 16), B along: the time is B's bytes, or latency where they are few (one
-// token, 4096 x 4096 in bf16: 7.5 us, 4.5 TB/s, against 8.7 + 4.8 us in tiles with shares). A
+// token, 4096 x 4096 in bf16: 8 us, 4.2 TB/s, against 8.7 + 4.8 us in tiles with shares). A
 // workgroup takes 16 columns, its waves every WAVES-th block each, fragments straight from memory
 // and several blocks at a time; the waves' sums meet in LDS, added in one order. Any address and
 // distance of rows is taken.
@@ -677,7 +677,7 @@ struct Plan {
 // tiles of much depth are cut into shares of ten blocks or more, up to two for a CU: 128 x 512 x
 // 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole. An fp32
 // tile takes its products' time, whatever its neighbours: between one and four for a CU, rows
-// are halved where that shares them out better (777 x 1500 x 1000, 312 tiles or 600: 40 us and 30).
+// are halved where that shares them out better (777 x 1500 x 1000, 312 tiles or 600: 41 us and 34).
 Plan plan_product(int64_t rows, int64_t cols, int64_t depth, int64_t size) {
   const int64_t block = 128 / size, blocks = (depth + block - 1) / block;
   Plan p = {64, 1, (blocks > 0 ? blocks : 1) * block};

@@ -414,20 +414,19 @@ constexpr int kSums = 5;
 
 // A workgroup goes through one chunk of a worker's rows (up to 8 * THREADS * NV columns), its
 // share of the parameters' gradients in registers, and writes that to `partial`;
-// k_residual_sums adds the chunks of a worker. R rows are worked on at a time, with one
-// barrier for each norm's sums, while the next R are on their way. bf16 32768 x 4096 of 19 workers
-// 290 us and 7 for the sums, 16384 x 8192 470 (all sums in registers, of which two thirds then are
-// in scratch: 640).
-// HOLD: the parameters and all sums stay in registers and the next rows' ds and gate come early
-// too; else the parameters are read again for every R rows, ds and the gate come under the first
+// k_residual_sums adds the chunks of a worker. One barrier for each norm's sums, while the next
+// row is on its way. bf16 32768 x 4096 of 19 workers 290 us and 7 for the sums, 16384 x 8192 470 (all
+// sums in registers, of which two thirds then are in scratch: 640).
+// HOLD: the parameters and all sums stay in registers and the next row's ds and gate come early
+// too; else the parameters are read again for every row, ds and the gate come under the first
 // norm's sums, and all sums but the first live in LDS, each thread's own values.
-template <typename T, int THREADS, int NV, int R, bool HOLD>
+template <typename T, int THREADS, int NV, bool HOLD>
 __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackward a,
                                                                Chunks chunks, int sums_of,
                                                                float* partial) {
   constexpr int kWaves = THREADS / 64;
   typedef typename Pack8<T>::type Raw;
-  __shared__ float sums[2][2][kWaves][2 * R];
+  __shared__ float sums[2][2][kWaves][2];
   constexpr int kHeld = HOLD ? kSums : 1;  // sums in registers
   __shared__ v4f totals[HOLD ? 1 : kSums - 1][NV][2][HOLD ? 1 : THREADS];
   const garfield_residual_block& b = a.b;
@@ -485,182 +484,146 @@ __global__ __launch_bounds__(THREADS) void k_residual_backward(ResidualNormBackw
       }
     }
   };
-  Raw ds[R][NV], dy[R][NV], s[R][NV], h[R][NV], gate[R][NV];
-  float mean[R], rstd[R], post_mean[R], post_rstd[R];
+  Raw ds[NV], dy[NV], s[NV], h[NV], gate[NV];
+  float mean = 0.0f, rstd = 1.0f, post_mean = 0.0f, post_rstd = 1.0f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    mean[r] = post_mean[r] = 0.0f;
-    rstd[r] = post_rstd[r] = 1.0f;
+  for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int e = 0; e < 8; ++e) ds[j][e] = dy[j][e] = s[j][e] = static_cast<T>(0.0f);
+  auto fetch = [&](int64_t row) {
+    if (a.dy) {
+      if (!b.rms) mean = a.mean[row];
+      rstd = a.rstd[row];
+    }
+    if (post) {
+      if (!b.rms) post_mean = a.post_mean[row];
+      post_rstd = a.post_rstd[row];
+    }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ds[r][j][e] = dy[r][j][e] = s[r][j][e] = static_cast<T>(0.0f);
-  }
-  auto fetch = [&](int64_t row0) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = row0 + r < end ? row0 + r : end - 1;
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+      auto of = [&](const void* p, int64_t ld) {
+        return raw8_upto(static_cast<const T*>(p) + row * ld + c, left);
+      };
       if (a.dy) {
-        if (!b.rms) mean[r] = a.mean[row];
-        rstd[r] = a.rstd[row];
+        dy[j] = of(a.dy, a.lddy);
+        s[j] = of(a.s, a.lds);
       }
-      if (post) {
-        if (!b.rms) post_mean[r] = a.post_mean[row];
-        post_rstd[r] = a.post_rstd[row];
-      }
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
-        auto of = [&](const void* p, int64_t ld) {
-          return raw8_upto(static_cast<const T*>(p) + row * ld + c, left);
-        };
-        if (a.dy) {
-          dy[r][j] = of(a.dy, a.lddy);
-          s[r][j] = of(a.s, a.lds);
-        }
-        h[r][j] = of(a.h, a.ldh);
-        if constexpr (HOLD) {
-          if (a.ds) ds[r][j] = of(a.ds, a.ldds);
-          if (by_tokens) gate[r][j] = of(b.gate, b.ld_gate);
-        }
+      h[j] = of(a.h, a.ldh);
+      if constexpr (HOLD) {
+        if (a.ds) ds[j] = of(a.ds, a.ldds);
+        if (by_tokens) gate[j] = of(b.gate, b.ld_gate);
       }
     }
   };
-  auto fetch_late = [&](int64_t row0) {
+  auto fetch_late = [&](int64_t row) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t row = row0 + r < end ? row0 + r : end - 1;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
-        if (a.ds) ds[r][j] = raw8_upto(static_cast<const T*>(a.ds) + row * a.ldds + c, left);
-        if (by_tokens)
-          gate[r][j] = raw8_upto(static_cast<const T*>(b.gate) + row * b.ld_gate + c, left);
-      }
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+      if (a.ds) ds[j] = raw8_upto(static_cast<const T*>(a.ds) + row * a.ldds + c, left);
+      if (by_tokens)
+        gate[j] = raw8_upto(static_cast<const T*>(b.gate) + row * b.ld_gate + c, left);
     }
   };
   fetch(begin);
-  for (int64_t row0 = begin; row0 < end; row0 += R) {
-    const int odd = (row0 - begin) / R & 1;  // the sums alternate between two places
-    float g[R][NV][8], hat[R][NV][8], z[R][NV][8], k[R][NV][8], both[2 * R], d[R], pd[R];
+  for (int64_t row = begin; row < end; ++row) {
+    const int odd = (row - begin) & 1;  // the sums alternate between two places
+    float g[NV][8], hat[NV][8], z[NV][8], k[NV][8], both[2];
+    const float d = rstd, pd = post_rstd;
     if constexpr (!HOLD) {
       parameter(b.weight, 0.0f, w);
-      fetch_late(row0);
+      fetch_late(row);
     }
+    both[0] = both[1] = 0.0f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool there = r == 0 || row0 + r < end;
-      float along = 0.0f, across = 0.0f;
-      d[r] = rstd[r];
-      pd[r] = post_rstd[r];
+    for (int j = 0; j < NV; ++j) {
+      const int64_t left = b.cols - (j * THREADS + threadIdx.x) * 8;
+      unpack8<T>(dy[j], g[j]);
+      unpack8<T>(s[j], hat[j]);
+      unpack8<T>(h[j], z[j]);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int64_t left = b.cols - (j * THREADS + threadIdx.x) * 8;
-        unpack8<T>(dy[r][j], g[r][j]);
-        unpack8<T>(s[r][j], hat[r][j]);
-        unpack8<T>(h[r][j], z[r][j]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          hat[r][j][e] = (hat[r][j][e] - mean[r]) * d[r];
-          if (post) z[r][j][e] = (z[r][j][e] - post_mean[r]) * pd[r];
-          if (left < 8 && e >= left) hat[r][j][e] = z[r][j][e] = 0.0f;
-        }
-        if (there) {
-          add(0, j, g[r][j], hat[r][j]);
-          if (HOLD || sums_of & 2) add(1, j, g[r][j], nullptr);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          g[r][j][e] *= w[j][e];
-          along += g[r][j][e];
-          across = __builtin_fmaf(g[r][j][e], hat[r][j][e], across);
-        }
+      for (int e = 0; e < 8; ++e) {
+        hat[j][e] = (hat[j][e] - mean) * d;
+        if (post) z[j][e] = (z[j][e] - post_mean) * pd;
+        if (left < 8 && e >= left) hat[j][e] = z[j][e] = 0.0f;
       }
-      both[2 * r] = along;
-      both[2 * r + 1] = across;
+      add(0, j, g[j], hat[j]);
+      if (HOLD || sums_of & 2) add(1, j, g[j], nullptr);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        g[j][e] *= w[j][e];
+        both[0] += g[j][e];
+        both[1] = __builtin_fmaf(g[j][e], hat[j][e], both[1]);
+      }
     }
-    // ds and the gate go on to the whole gradient, and the next rows come
-    float more[R][NV][8];
+    // ds and the gate go on to the whole gradient, and the next row comes
+    float more[NV][8];
     auto go_on = [&] {
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+      for (int j = 0; j < NV; ++j) {
+        unpack8<T>(ds[j], more[j]);
+        if (by_tokens) {
+          unpack8<T>(gate[j], k[j]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          unpack8<T>(ds[r][j], more[r][j]);
-          if (by_tokens) {
-            unpack8<T>(gate[r][j], k[r][j]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) k[r][j][e] = gv[j][e];
-          }
+          for (int e = 0; e < 8; ++e) k[j][e] = gv[j][e];
         }
+      }
     };
     if constexpr (HOLD) go_on();
-    if (row0 + R < end) fetch(row0 + R);
-    if (a.dy) sums_group<kWaves, 2 * R>(both, sums[0][odd]);
+    if (row + 1 < end) fetch(row + 1);
+    if (a.dy) sums_group<kWaves, 2>(both, sums[0][odd]);
     if constexpr (!HOLD) {
       parameter(columns, 1.0f, gv);
       go_on();
       parameter(b.post_weight, 1.0f, pw);
       parameter(b.post_bias, 0.0f, pb);
     }
+    const float along = b.rms || !a.dy ? 0.0f : both[0] * scale;
+    const float across = a.dy ? both[1] * scale : 0.0f;
+    both[0] = both[1] = 0.0f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool there = r == 0 || row0 + r < end;
-      const float along = b.rms || !a.dy ? 0.0f : both[2 * r] * scale;
-      const float across = a.dy ? both[2 * r + 1] * scale : 0.0f;
-      float x = 0.0f, y = 0.0f;
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+      float f[8];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v = more[r][j][e];
-          if (a.dy) v += d[r] * (g[r][j][e] - along - hat[r][j][e] * across);
-          if (left < 8 && e >= left) v = 0.0f;
-          g[r][j][e] = v;
-          f[e] = post ? __builtin_fmaf(z[r][j][e], pw[j][e], pb[j][e]) : z[r][j][e];
-          f[e] *= v;
-          k[r][j][e] *= v;  // the gradient of N_post(h)
-        }
-        if (there) {
-          if (HOLD || sums_of & 4) add(2, j, k[r][j], z[r][j]);
-          if (HOLD || sums_of & 8) add(3, j, k[r][j], nullptr);
-          if (HOLD || sums_of & 16) add(4, j, f, nullptr);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (post) {
-            k[r][j][e] *= pw[j][e];
-            x += k[r][j][e];
-            y = __builtin_fmaf(k[r][j][e], z[r][j][e], y);
-          }
-          g[r][j][e] *= b.scale;
-        }
-        if (there && left > 0) {
-          if (a.dx) store8_upto(static_cast<T*>(a.dx) + (row0 + r) * a.lddx + c, left, g[r][j]);
-          if (a.dgate) store8_upto(static_cast<T*>(a.dgate) + (row0 + r) * a.lddgate + c, left, f);
-        }
+      for (int e = 0; e < 8; ++e) {
+        float v = more[j][e];
+        if (a.dy) v += d * (g[j][e] - along - hat[j][e] * across);
+        if (left < 8 && e >= left) v = 0.0f;
+        g[j][e] = v;
+        f[e] = post ? __builtin_fmaf(z[j][e], pw[j][e], pb[j][e]) : z[j][e];
+        f[e] *= v;
+        k[j][e] *= v;  // the gradient of N_post(h)
       }
-      both[2 * r] = x;
-      both[2 * r + 1] = y;
+      if (HOLD || sums_of & 4) add(2, j, k[j], z[j]);
+      if (HOLD || sums_of & 8) add(3, j, k[j], nullptr);
+      if (HOLD || sums_of & 16) add(4, j, f, nullptr);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (post) {
+          k[j][e] *= pw[j][e];
+          both[0] += k[j][e];
+          both[1] = __builtin_fmaf(k[j][e], z[j][e], both[1]);
+        }
+        g[j][e] *= b.scale;
+      }
+      if (left > 0) {
+        if (a.dx) store8_upto(static_cast<T*>(a.dx) + row * a.lddx + c, left, g[j]);
+        if (a.dgate) store8_upto(static_cast<T*>(a.dgate) + row * a.lddgate + c, left, f);
+      }
     }
     if (!a.dh) continue;
-    if (post) sums_group<kWaves, 2 * R>(both, sums[1][odd]);
+    if (post) sums_group<kWaves, 2>(both, sums[1][odd]);
+    const float x = b.rms ? 0.0f : both[0] * scale, y = both[1] * scale;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (r > 0 && row0 + r >= end) break;
-      const float x = b.rms ? 0.0f : both[2 * r] * scale, y = both[2 * r + 1] * scale;
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
+      if (post) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int64_t c = (j * THREADS + threadIdx.x) * 8, left = b.cols - c;
-        if (post) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) k[r][j][e] = pd[r] * (k[r][j][e] - x - z[r][j][e] * y);
-        }
-        if (left > 0) store8_upto(static_cast<T*>(a.dh) + (row0 + r) * a.lddh + c, left, k[r][j]);
+        for (int e = 0; e < 8; ++e) k[j][e] = pd * (k[j][e] - x - z[j][e] * y);
       }
+      if (left > 0) store8_upto(static_cast<T*>(a.dh) + row * a.lddh + c, left, k[j]);
     }
   }
   int rank = 0;
@@ -760,9 +723,9 @@ int sums_asked(const garfield_residual_gradients& to) {
 
 constexpr int64_t kBackwardMaxCols = 8192;
 
-template <typename T, int THREADS, int NV, int R, bool HOLD = true>
+template <typename T, int THREADS, int NV, bool HOLD = true>
 void launch_backward(const ResidualNormBackward& a, const Chunks& c, float* partial, hipStream_t s) {
-  launch("residual_backward", k_residual_backward<T, THREADS, NV, R, HOLD>, dim3(c.chunk0[c.n]),
+  launch("residual_backward", k_residual_backward<T, THREADS, NV, HOLD>, dim3(c.chunk0[c.n]),
          dim3(THREADS), 0, s, a, c, sums_asked(a.to), partial);
 }
 
@@ -781,15 +744,15 @@ void choose_backward(const ResidualNormBackward& a, const Chunks& c, void* works
                dim3(static_cast<uint32_t>((cols + 511) / 512), c.chunk0[c.n]), dim3(64), 0, s, a, c,
                means, sums, partial);
     } else if (cols > 4096) {
-      launch_backward<T, 512, 2, 1, false>(a, c, partial, s);
+      launch_backward<T, 512, 2, false>(a, c, partial, s);
     } else if (cols > 2048) {
-      launch_backward<T, 512, 1, 1>(a, c, partial, s);
+      launch_backward<T, 512, 1>(a, c, partial, s);
     } else if (cols > 1024) {
-      launch_backward<T, 256, 1, 1>(a, c, partial, s);
+      launch_backward<T, 256, 1>(a, c, partial, s);
     } else if (cols > 512) {
-      launch_backward<T, 128, 1, 1>(a, c, partial, s);
+      launch_backward<T, 128, 1>(a, c, partial, s);
     } else {
-      launch_backward<T, 64, 1, 1>(a, c, partial, s);
+      launch_backward<T, 64, 1>(a, c, partial, s);
     }
   }
   if (sums) {

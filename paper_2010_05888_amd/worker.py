@@ -737,7 +737,8 @@ def clip_gradients(grads, max_norm: float, out: torch.Tensor | None = None) -> t
     """Clip each worker's gradient to max_norm: all its tensors' values times max_norm / norm
     where its norm over all of them is larger. In place, or with out (n x d, float32) the
     tensors one after the other into the workers' rows of out, e.g. the matrix that the rules
-    take; out shares no memory with them. Returns the norms before (float32). grads as for gradient_norms()."""
+    take; out shares no memory with them. Returns the norms before (float32). grads as for
+    gradient_norms()."""
     count, n, held, dev, d = _tensors(grads)
     if not max_norm >= 0:
         raise ValueError("max_norm must be 0 or more")
