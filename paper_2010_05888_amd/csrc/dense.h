@@ -75,8 +75,8 @@ struct Side {
   const char* at;        // of the block that comes next
   int64_t step;          // bytes between blocks
   uint32_t ld;           // bytes between rows
-  uint32_t last;         // across: bytes of the last row that are read
-  uint32_t bytes;        // along: from a block's first line to its last one
+  uint32_t last;         // bytes of the last row that are read
+  uint32_t bytes;        // along: of a block, from its first line's to the last line's end
   uint32_t of[kLoads];   // the lane's place in each load
   int deep;              // along: the depth at which the lane's piece starts
 
@@ -102,8 +102,8 @@ struct Side {
       }
     } else {
       step = 128;
-      last = 0;
-      bytes = (here - 1) * ld;
+      last = 128;
+      bytes = (here - 1) * ld + (ld < 128 ? ld : 128);  // the next line is not there
       const int chunk = piece ^ ((wave * 8 + row) / 2 % 8);  // that of lines 16 n on too
       deep = chunk * 16 / kSize;
 #pragma unroll
@@ -113,13 +113,9 @@ struct Side {
 
   // The next block, of which `left` depths are there (none: it reads as 0).
   __device__ __forceinline__ u4 next(int left) {
-    const int deep_now = left < kDepth ? left : kDepth;
-    uint32_t there = 0;
-    if (left > 0) {
-      if constexpr (ACROSS) there = (deep_now - 1) * ld + last;
-      // to the last depth's piece: rows shorter than a block have the lines past the last one there
-      else there = bytes + (deep_now * kSize + 15) / 16 * 16;
-    }
+    uint32_t there = bytes;
+    if constexpr (ACROSS)
+      there = left <= 0 ? 0 : ((left < kDepth ? left : kDepth) - 1) * ld + last;
     const u4 b = buffer_of(at, there);
     at += step;
     return b;
