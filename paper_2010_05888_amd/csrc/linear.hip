@@ -676,31 +676,48 @@ struct Plan {
   int64_t share;  // depths
 };
 
-// The largest tile of which there are 192 (of 256 CUs): in bf16 3500 x 3500 x 2000, 196 tiles of
-// 256 x 256, takes 66 us and 76 in tiles of 128; 2048 x 4096 x 4096, 128 of 256, takes 64 in tiles
-// of 128 and 84 in those; 1000 x 2000 x 3000, 512 of 64, 30 in tiles of 64 and 43 in 128. Few
-// tiles of much depth are cut into shares of ten blocks or more, up to two for a CU: 128 x 512 x
-// 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole. An fp32
-// tile takes its products' time, whatever its neighbours: between one and four for a CU, rows
-// are halved where that shares them out better (777 x 1500 x 1000, 312 tiles or 600: 41 us and 34).
+// The fp32 tiles, of n matrices, with the least work for the busiest CU: a tile takes its products'
+// time, whatever its neighbours, small ones 5 and 12% more an output, large ones 5% less (6724 x
+// 2560 x 1808, 270 tiles of 256 or 4240 of 64: 851 us and 477; 777 x 1500 x 1000, 312 of 64 or 600 of
+// 32: 41 and 34).
+int least_work(int64_t rows, int64_t cols, int64_t n, bool halves) {
+  const int64_t cus = device_cus();
+  int64_t least = INT64_MAX;
+  int size = 64;
+  auto weigh = [&](int tile, int64_t tiles, int64_t outputs, int64_t percent) {
+    const int64_t work = (tiles * n + cus - 1) / cus * outputs * percent;
+    if (work < least) {
+      least = work;
+      size = tile;
+    }
+  };
+  weigh(256, tiles_of(rows, cols, 256), 256 * 256, 95);
+  weigh(128, tiles_of(rows, cols, 128), 128 * 128, 100);
+  weigh(64, tiles_of(rows, cols, 64), 64 * 64, 105);
+  if (halves) weigh(32, (rows + 31) / 32 * ((cols + 63) / 64), 32 * 64, 112);
+  return size;
+}
+
+// Few tiles of much depth are cut into shares of ten blocks or more, up to two for a CU: in bf16 128
+// x 512 x 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole. Else
+// 16-bit products take the largest tile of which there are 192 (of 256 CUs): 3500 x 3500 x 2000,
+// 196 tiles of 256 x 256, 66 us and 76 in tiles of 128; 2048 x 4096 x 4096, 128 of 256, 64 in tiles of
+// 128 and 84 in those; 1000 x 2000 x 3000, 512 of 64, 30 in tiles of 64 and 43 in 128.
 Plan plan_product(int64_t rows, int64_t cols, int64_t depth, int64_t size) {
   const int64_t block = 128 / size, blocks = (depth + block - 1) / block;
   Plan p = {64, 1, (blocks > 0 ? blocks : 1) * block};
   const int64_t cus = device_cus(), tiles = tiles_of(rows, cols, 64);
-  if (tiles_of(rows, cols, 256) >= cus * 3 / 4) {
+  const int64_t want = tiles > 0 ? std::min(2 * cus / tiles, blocks / 10) : 1;
+  if (want >= 2) {
+    const int64_t per = (blocks + want - 1) / want;
+    p.share = per * block;
+    p.shares = static_cast<int>((blocks + per - 1) / per);
+  } else if (size == 4) {
+    p.size = least_work(rows, cols, 1, true);
+  } else if (tiles_of(rows, cols, 256) >= cus * 3 / 4) {
     p.size = 256;
   } else if (tiles_of(rows, cols, 128) >= cus * 3 / 4) {
     p.size = 128;
-  } else if (tiles > 0) {
-    const int64_t want = std::min(2 * cus / tiles, blocks / 10);
-    if (want >= 2) {
-      const int64_t per = (blocks + want - 1) / want;
-      p.share = per * block;
-      p.shares = static_cast<int>((blocks + per - 1) / per);
-    } else if (size == 4 && tiles > cus) {
-      const int64_t halves = (rows + 31) / 32 * ((cols + 63) / 64);
-      if ((halves + cus - 1) / cus < 2 * ((tiles + cus - 1) / cus)) p.size = 32;
-    }
   }
   return p;
 }
@@ -794,13 +811,12 @@ void launch_product(const Product& p, void* workspace, hipStream_t s) {
 Plan plan_gradient(const DenseGradient& a, int64_t size) {
   const int64_t block = 128 / size, blocks = (a.tokens / a.n + block - 1) / block;
   Plan p = {64, 1, 0};
-  if (tiles_of(a.outputs, a.inputs, 256) * a.n >= 192) p.size = 256;
+  const int64_t tiles = tiles_of(a.outputs, a.inputs, 64) * a.n;
+  const int64_t want = tiles > 0 ? std::min(3 * int64_t{device_cus()} / tiles, blocks / 4) : 1;
+  if (size == 4 && want < 2) p.size = least_work(a.outputs, a.inputs, a.n, false);
+  else if (tiles_of(a.outputs, a.inputs, 256) * a.n >= 192) p.size = 256;
   else if (tiles_of(a.outputs, a.inputs, 128) * a.n >= 192) p.size = 128;
-  else if (a.outputs > 0 && a.inputs > 0) {
-    const int64_t tiles = tiles_of(a.outputs, a.inputs, 64) * a.n, most = 3 * int64_t{device_cus()};
-    const int64_t want = std::min(most / tiles, blocks / 4);
-    if (want >= 2) p.shares = static_cast<int>(std::min<int64_t>(want, 16));
-  }
+  else if (want >= 2) p.shares = static_cast<int>(std::min<int64_t>(want, 16));
   return p;
 }
 

@@ -37,10 +37,10 @@ def _check(got, want, dtype, what):
     assert bool(got.isfinite().all()) and float(over.max()) <= 0, (what, float(over.max()))
 
 
-# (rows, columns, depth) of: tiles of 256 (225 of them), of 128 (210), of 64 (uncut: 320), of 32 in
+# (rows, columns, depth) of: tiles of 256 (256 of them, 225), of 128 (256, 210), of 64 (uncut: 320), of 32 in
 # fp32 (600), shares (80 tiles, 16, 2), few rows, a depth below a block, and one of a whole number
-PRODUCTS = [(3700, 3650, 200), (3700, 3656, 1032), (1800, 1750, 136), (1795, 1750, 600), (1000, 1250, 330),
-            (777, 1500, 1000), (300, 1000, 4096), (120, 500, 8192), (40, 100, 3000), (16, 1000, 4104),
+PRODUCTS = [(4090, 4081, 200), (2040, 2030, 330), (3700, 3650, 200), (3700, 3656, 1032), (1800, 1750, 136),
+            (1795, 1750, 600), (1000, 1250, 330), (777, 1500, 1000), (300, 1000, 4096), (120, 500, 8192), (40, 100, 3000), (16, 1000, 4104),
             (15, 1003, 4100), (9, 33, 700), (300, 300, 8), (700, 640, 64)]
 
 
@@ -65,8 +65,8 @@ def test_products_of_each_form(m, n, k, dtype, layout):
 
 
 # (workers, tokens, outputs, inputs): tiles of 256, 128 and 64, shares of the tokens, whole lines and not
-GRADIENTS = [(12, 1500, 1000, 1030), (12, 1500, 1000, 1024), (19, 700, 300, 500), (19, 700, 320, 512),
-             (3, 400, 130, 200), (1, 3000, 200, 300), (2, 5001, 70, 64), (60, 130, 512, 256), (1, 100, 8, 2000)]
+GRADIENTS = [(16, 900, 1020, 1010), (16, 900, 500, 510), (12, 1500, 1000, 1030), (12, 1500, 1000, 1024), (19, 700, 300, 500),
+             (19, 700, 320, 512), (3, 400, 130, 200), (1, 3000, 200, 300), (2, 5001, 70, 64), (60, 130, 512, 256), (1, 100, 8, 2000)]
 
 
 @pytest.mark.parametrize("layout", ["plain", "apart", "strided", "offset"])
