@@ -676,33 +676,33 @@ struct Plan {
   int64_t share;  // depths
 };
 
-// The fp32 tiles, of n matrices, with the least work for the busiest CU: a tile takes its products'
-// time, whatever its neighbours, small ones 5 and 12% more an output, large ones 5% less (6724 x
-// 2560 x 1808, 270 tiles of 256 or 4240 of 64: 851 us and 477; 777 x 1500 x 1000, 312 of 64 or 600 of
-// 32: 41 and 34).
-int least_work(int64_t rows, int64_t cols, int64_t n, bool halves) {
+// The tiles, of n matrices, with the least work for the busiest CU, an output of small tiles weighed
+// as more. An fp32 tile takes its products' time, whatever its neighbours (6724 x 2560 x 1808, 270
+// tiles of 256 or 4240 of 64: 851 us and 477; 777 x 1500 x 1000, 312 of 64 or 600 of 32: 41 and 34). One
+// of 16 bits is bound by what it reads, too: 7476 x 1104 x 3984 in bf16, 150 tiles of 256 or 531 of
+// 128, 94 us and 130; 2048 x 4096 x 4096, 128 of 256 or 512 of 128, 84 and 64; 1000 x 2000 x 3000, 128 of
+// 128 or 512 of 64, 43 and 30; 18 workers' 879 x 3600 x 128, 270 of 256 or 1026 of 64, 17 and 12.
+int least_work(int64_t rows, int64_t cols, int64_t n, int64_t size, bool halves) {
   const int64_t cus = device_cus();
   int64_t least = INT64_MAX;
-  int size = 64;
+  int best = 64;
   auto weigh = [&](int tile, int64_t tiles, int64_t outputs, int64_t percent) {
     const int64_t work = (tiles * n + cus - 1) / cus * outputs * percent;
     if (work < least) {
       least = work;
-      size = tile;
+      best = tile;
     }
   };
-  weigh(256, tiles_of(rows, cols, 256), 256 * 256, 95);
-  weigh(128, tiles_of(rows, cols, 128), 128 * 128, 100);
-  weigh(64, tiles_of(rows, cols, 64), 64 * 64, 105);
+  const bool f32 = size == 4;
   if (halves) weigh(32, (rows + 31) / 32 * ((cols + 63) / 64), 32 * 64, 112);
-  return size;
+  weigh(64, tiles_of(rows, cols, 64), 64 * 64, f32 ? 105 : 200);
+  weigh(128, tiles_of(rows, cols, 128), 128 * 128, 100);
+  weigh(256, tiles_of(rows, cols, 256), 256 * 256, f32 ? 95 : 65);
+  return best;
 }
 
 // Few tiles of much depth are cut into shares of ten blocks or more, up to two for a CU: in bf16 128
-// x 512 x 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole. Else
-// 16-bit products take the largest tile of which there are 192 (of 256 CUs): 3500 x 3500 x 2000,
-// 196 tiles of 256 x 256, 66 us and 76 in tiles of 128; 2048 x 4096 x 4096, 128 of 256, 64 in tiles of
-// 128 and 84 in those; 1000 x 2000 x 3000, 512 of 64, 30 in tiles of 64 and 43 in 128.
+// x 512 x 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole.
 Plan plan_product(int64_t rows, int64_t cols, int64_t depth, int64_t size) {
   const int64_t block = 128 / size, blocks = (depth + block - 1) / block;
   Plan p = {64, 1, (blocks > 0 ? blocks : 1) * block};
@@ -712,12 +712,8 @@ Plan plan_product(int64_t rows, int64_t cols, int64_t depth, int64_t size) {
     const int64_t per = (blocks + want - 1) / want;
     p.share = per * block;
     p.shares = static_cast<int>((blocks + per - 1) / per);
-  } else if (size == 4) {
-    p.size = least_work(rows, cols, 1, true);
-  } else if (tiles_of(rows, cols, 256) >= cus * 3 / 4) {
-    p.size = 256;
-  } else if (tiles_of(rows, cols, 128) >= cus * 3 / 4) {
-    p.size = 128;
+  } else {
+    p.size = least_work(rows, cols, 1, size, size == 4);
   }
   return p;
 }
@@ -813,10 +809,8 @@ Plan plan_gradient(const DenseGradient& a, int64_t size) {
   Plan p = {64, 1, 0};
   const int64_t tiles = tiles_of(a.outputs, a.inputs, 64) * a.n;
   const int64_t want = tiles > 0 ? std::min(3 * int64_t{device_cus()} / tiles, blocks / 4) : 1;
-  if (size == 4 && want < 2) p.size = least_work(a.outputs, a.inputs, a.n, false);
-  else if (tiles_of(a.outputs, a.inputs, 256) * a.n >= 192) p.size = 256;
-  else if (tiles_of(a.outputs, a.inputs, 128) * a.n >= 192) p.size = 128;
-  else if (want >= 2) p.shares = static_cast<int>(std::min<int64_t>(want, 16));
+  if (want >= 2) p.shares = static_cast<int>(std::min<int64_t>(want, 16));
+  else p.size = least_work(a.outputs, a.inputs, a.n, size, false);
   return p;
 }
 
