@@ -142,8 +142,8 @@ struct Tile {
   static constexpr int kLoads = SideA::kLoads + SideB::kLoads;
   static constexpr int kDepth = SideA::kDepth;
   // Blocks in LDS or on their way. Three of small tiles in 16 bits: 512 x 4096 x 4096 takes 29 us so
-  // and 33 in two, other sizes up to 4% less or more; fp32 tiles, which wait for their products, are 3 to
-  // 5% slower in three, weight gradients 2%.
+  // and 33 in two, other sizes up to 4% less or more; fp32 tiles, which wait for their products,
+  // are 3 to 5% slower in three, weight gradients 2%.
   static constexpr int kStages = sizeof(T) == 2 && !AA && kRows * kCols <= 64 * 64 ? 3 : 2;
   static constexpr int kLds = kStages * kStage;
 
