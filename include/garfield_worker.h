@@ -163,7 +163,8 @@ garfield_status garfield_weight_gradient(const void* dy, int type, int64_t token
 /* What is done with a linear layer's sums. */
 typedef enum garfield_activation {
   GARFIELD_NO_ACTIVATION = 0,
-  GARFIELD_RELU = 1,      /* max(p, 0); its slope at 0 is 0 */
+  GARFIELD_RELU = 1,      /* max(p, 0); a gradient passes where p > 0 and is 0 elsewhere,
+                             whatever it was */
   GARFIELD_GELU = 2,      /* p Phi(p), Phi the normal distribution's */
   GARFIELD_GELU_TANH = 3, /* p (1 + tanh(sqrt(2 / pi) (p + 0.044715 p^3))) / 2 */
   GARFIELD_SILU = 4       /* p / (1 + exp(-p)) */

@@ -91,13 +91,14 @@ __device__ __forceinline__ float silu_slope(float p) {
   return __builtin_fmaf(p, e * q * q, q);
 }
 
-// v times the slopes at p.
+// v times the slopes at p; relu's is 0 or 1, and chosen: where it is 0 nothing of v gets on, not an
+// infinity either.
 template <int N>
 __device__ __forceinline__ void times_slope(int activation, const float* p, float* v) {
   switch (activation) {
     case GARFIELD_RELU:
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] *= p[e] > 0.0f ? 1.0f : 0.0f;
+      for (int e = 0; e < N; ++e) v[e] = p[e] > 0.0f ? v[e] : 0.0f;
       break;
     case GARFIELD_GELU:
 #pragma unroll
