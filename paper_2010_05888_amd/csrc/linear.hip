@@ -273,6 +273,7 @@ struct Tile {
         for (int i = 0; i < FA; ++i)
           *reinterpret_cast<v4f*>(own + place(i * 4 + lane / 16, k * 16 + lane % 16)) =
               sum[i][k0 + k];
+      wave_exchange();
 #pragma unroll 1
       for (int r0 = first; r0 < kPass * 16; r0 += kAsked * kApart) {
 #pragma unroll
@@ -299,6 +300,7 @@ struct Tile {
           put(now, line, column, t);
         }
       }
+      wave_exchange();
     }
   }
 };

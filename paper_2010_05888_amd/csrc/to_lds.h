@@ -84,4 +84,13 @@ __device__ __forceinline__ void barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
 }
 
+// Between accesses to LDS by which the lanes of one wave give each other values: what any of them
+// did before is done for all of them after. The hardware keeps a wave's accesses in order, so
+// this is no instruction; it keeps the compiler from putting them in another order.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 }  // namespace garfield

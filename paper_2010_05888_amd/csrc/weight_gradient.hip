@@ -365,6 +365,7 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
 #pragma unroll
       for (int i = 0; i < kFA; ++i)
         *reinterpret_cast<v4f*>(own + lane % 16 * kRow + i * 64 + lane / 16 * 16) = sum[i][k];
+      wave_exchange();
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         const int row = r + lane / 32;
@@ -385,6 +386,7 @@ __global__ __launch_bounds__(256 * WK, 2) void k_weight_gradient(
             if (e < left_k) to[e] = t[e];
         }
       }
+      wave_exchange();
     }
   };
   if (whole_lines) store(std::true_type());
