@@ -73,9 +73,11 @@ __device__ __forceinline__ void activate(int activation, float* v) {
 
 // (p q(u))' = q + p u' q (1 - q), 1 - q = e q. p is kept where e and p u' are finite; beyond
 // that the slopes are 0 and 1. gelu's p, of which only an infinite one must not meet the density's
-// 0, is kept to 1e18, far beyond where the density is 0.
+// 0, is kept to 1e18, far beyond where the density is 0; the density's factor (2 pi)^(-1/2) is in
+// its exponent, which makes up for that instruction.
 __device__ __forceinline__ float gelu_slope(float p) {
-  const float density = 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.5f * kLog2e * (p * p));
+  const float density =
+      __builtin_amdgcn_exp2f(__builtin_fmaf(p * p, -0.5f * kLog2e, -1.3257480647361592f));
   return __builtin_fmaf(__builtin_amdgcn_fmed3f(p, -1e18f, 1e18f), density,
                         logistic(exp_minus(normal_argument(p))));
 }
