@@ -300,9 +300,9 @@ typedef struct garfield_gradient {
  * the tensors one after the other into worker w's row of fp32 values at out + w * ld_out, or
  * in place with out NULL (values are then rounded once to their type). What is written must
  * share no memory with another tensor, or with any with out (GARFIELD_EINVAL). Squares are added
- * up in 64 bits. A worker with an infinite value gets zeros and, for the infinities, NaN; one with
- * a NaN gets NaN throughout: norms says which. At most 2^20 tensors, each of at most 2^34 values
- * a worker (GARFIELD_ETOOBIG).
+ * up in 64 bits. A worker with an infinite value gets zeros and, for the infinities, NaN (with
+ * max_norm infinite its values as they are); one with a NaN gets NaN throughout: norms says which.
+ * At most 2^20 tensors, each of at most 2^34 values a worker (GARFIELD_ETOOBIG).
  */
 size_t garfield_clip_workspace(const garfield_gradient* tensors, int count, int n);
 garfield_status garfield_gradient_norms(const garfield_gradient* tensors, int count, int n,

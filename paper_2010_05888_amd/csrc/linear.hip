@@ -6,10 +6,12 @@
 // its depth. Products are those of the values as they are, sums fp32: fp32 on its own matrix
 // instruction, at a sixteenth of the 16-bit ones' rate.
 //
-// Bounds: the matrix cores' rate, and power (8192^3 in bf16: 800 us, 1370 TFLOP/s; in fp32 7500
-// us, 147 TFLOP/s of 157), and then what an epilogue reads, computes and writes, which no products
-// hide: 16384 x 8192 x 2048 takes 475 us, with gelu and p 535, back through gelu 540, of which
-// 268 MB more at a copy's rate are 51. For one token B's bytes, for small sizes latency.
+// Bounds: the matrix cores' rate, and power (8192^3 in bf16: 800 to 860 us, 1280 to 1370 TFLOP/s; in
+// fp32 7500 to 7800 us, 141 to 147 TFLOP/s of 157), and then what an epilogue reads, computes and
+// writes, which no products hide: 16384 x 8192 x 2048 takes 465 to 485 us, with gelu and p 540 to
+// 570, back through gelu 540 to 580, of which 268 MB more at a copy's rate are 51. (Passes with
+// pauses; without, power holds a card back by up to 15% more. A comment's pairs are of one run.)
+// For one token B's bytes, for small sizes latency.
 
 #include <algorithm>
 #include <type_traits>
@@ -96,7 +98,7 @@ struct Finish {
 // Workgroup id to tile: workgroups go to the eight XCDs in turn, so an XCD's
 // share is made contiguous, and inside it four tiles of rows deep: the tiles that
 // an XCD has in work share their rows of both operands in its L2, and write next to each
-// other (eight deep, 16384 x 8192 x 2048 takes 484 us, so 470; weight gradients below).
+// other (eight deep, 16384 x 8192 x 2048 takes 484 us, so 465; weight gradients below).
 // `parts`: shares of the depth, or workers, whose tiles come one part after the other.
 struct Place {
   int64_t m, j;
@@ -126,7 +128,7 @@ struct Parts {
 // one half it reads the next one's operands, so that nothing but the one barrier of a block, in
 // its middle, is waited for: there the block has been read, and the one after the next starts on
 // its way to its place, a load between every few products, straight to LDS.
-// 8192^3 in bf16: 800 us, 1370 TFLOP/s (a library's product 705 to 790), of zeros 650 (530): power
+// 8192^3 in bf16: 800 to 860 us (a library's product 700 to 790), of zeros 650 to 700 (530 to 580): power
 // bounds both; the matrix cores are busy 74% of the time, what they wait for are the loads' issue
 // (100 us) and the barrier (50). LDS is read 29% of the time and no bank is waited for. What was
 // slower: waves of 128 x 128, one a SIMD (1220); a block's loads all in its first products (815);
@@ -525,9 +527,10 @@ __global__ __launch_bounds__(64 * WJ * WM) void k_dense_gradient(Job p, Workers 
       if (m < p.rows) dbias[at.part * ld_dbias + m] = ones[k][0];
     }
   }
-  // Whole lines go past the caches: with 19 workers' 16384 x 4096 x 4096 680 us by way of them and
-  // 600 past them, with 11 workers' 1000 tokens 180 and 144. (Lines of several tiles of one row
-  // next to each other matter too: four tiles deep 16384 x 2048 x 8192 takes 640, eight 680.)
+  // Whole lines go past the caches: with 19 workers' 16384 x 4096 x 4096 674 us by way of them and
+  // 596 past them, with 11 workers' 1000 x 4096 x 4096 176 and 148 (1000 x 2048 x 2048, which the
+  // caches hold, 48 and 51). (Lines of several tiles of one row next to each other matter too: four
+  // tiles deep 16384 x 2048 x 8192 takes 667, eight 700.)
   float* const out = dw + at.part * ld_dw + m0 * p.cols + j0;
   auto store = [&](auto past_caches) {
     Of::template rows_of<4, Nothing>(
@@ -683,7 +686,8 @@ struct Plan {
 // tiles of 256 or 4240 of 64: 851 us and 477; 777 x 1500 x 1000, 312 of 64 or 600 of 32: 41 and 34). One
 // of 16 bits is bound by what it reads, too: 7476 x 1104 x 3984 in bf16, 150 tiles of 256 or 531 of
 // 128, 94 us and 130; 2048 x 4096 x 4096, 128 of 256 or 512 of 128, 84 and 64; 1000 x 2000 x 3000, 128 of
-// 128 or 512 of 64, 43 and 30; 18 workers' 879 x 3600 x 128, 270 of 256 or 1026 of 64, 17 and 12.
+// 128 or 512 of 64, 43 and 30; 18 workers' 879 x 3600 x 128, 270 of 256 or 522 of 128, 17 and 13 (2052
+// of 64 would take 11).
 int least_work(int64_t rows, int64_t cols, int64_t n, int64_t size, bool halves) {
   const int64_t cus = device_cus();
   int64_t least = INT64_MAX;
@@ -703,8 +707,9 @@ int least_work(int64_t rows, int64_t cols, int64_t n, int64_t size, bool halves)
   return best;
 }
 
-// Few tiles of much depth are cut into shares of ten blocks or more, up to two for a CU: in bf16 128
-// x 512 x 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096 14.8 in six, 21.1 whole.
+// Few tiles of much depth are cut into equal shares of ten blocks or more, the last one of what is left,
+// up to two for a CU: in bf16 128 x 512 x 8192 takes 13.3 us in twelve, 37.8 whole, 300 x 1000 x 4096
+// 14.8 in six, 21.1 whole.
 Plan plan_product(int64_t rows, int64_t cols, int64_t depth, int64_t size) {
   const int64_t block = 128 / size, blocks = (depth + block - 1) / block;
   Plan p = {64, 1, (blocks > 0 ? blocks : 1) * block};
@@ -729,7 +734,7 @@ void launch_tiles(Job p, const Plan& plan, const Epilogue& to, hipStream_t s) {
 }
 
 // Whether the matrix's rows are whole lines, which are stored past the caches: 16384 x 8192 x 2048
-// with gelu and p takes 518 us so and 536 by way of them. Parts of lines stay for the others.
+// with gelu and p takes 557 us so and 559 to 575 by way of them. Parts of lines stay for the others.
 bool whole_lines(const void* p, int64_t ld, int64_t size) {
   return reinterpret_cast<uintptr_t>(p) % 128 == 0 && ld * size % 128 == 0;
 }

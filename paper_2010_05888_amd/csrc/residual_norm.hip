@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kLong) void k_residual_norm_long(ResidualNorm a) {
 
 // ---------------------------------------------------------------------------
 // Longer rows' backward pass: dx, dh and a gate of tokens from three reads of a row, then the
-// parameters' gradients by columns, from a fourth: 8192 x 12288 in bf16 710 us, 1.7 TB/s of what
+// parameters' gradients by columns, from a fourth: 8192 x 12288 in bf16 790 us, 1.5 TB/s of what
 // one read would take. (Arrays indexed by a loop that is not unrolled live in scratch: 3100.)
 // What it knows of eight columns of a row.
 struct Eight {

@@ -65,3 +65,20 @@ def test_sums_beyond_fp16_have_slopes_of_0_and_1(m, n, k, name):
     off = (got[:, ::3].double() - product[:, ::3].double()).abs() - 2.0 ** -10 * product[:, ::3].double().abs()
     assert float(off.max()) <= 2.0 ** -24
     assert float(got[:, 1::3].abs().max()) <= 2.0 ** -24  # of 0: within fp16's smallest step
+
+
+@pytest.mark.parametrize("lengths", [[40], [40, 0, 90_000]])
+def test_an_infinite_limit_clips_nothing(lengths):
+    """Also not where a norm is infinite; a NaN is its worker's all the same."""
+    grads = [_rand(4, k, 1 + k) if k else torch.empty(4, 0) for k in lengths]
+    grads[0][1, 3], grads[0][1, 4], grads[0][2, 5] = float("inf"), -float("inf"), float("nan")
+    here = [g.to(DEV) for g in grads]
+    want = torch.cat(grads, 1)
+    want[2] = float("nan")
+    out = torch.empty(4, sum(lengths), device=DEV)
+    norms = gf.clip_gradients(here, float("inf"), out=out)
+    assert norms.isinf().tolist() == [False, True, False, False] and bool(norms[2].isnan())
+    assert torch.equal(out.cpu().nan_to_num(7.0, posinf=8.0, neginf=9.0), want.nan_to_num(7.0, posinf=8.0, neginf=9.0))
+    gf.clip_gradients(here, float("inf"))
+    assert torch.equal(torch.cat(here, 1).cpu().nan_to_num(7.0, posinf=8.0, neginf=9.0),
+                       want.nan_to_num(7.0, posinf=8.0, neginf=9.0))
